@@ -30,6 +30,22 @@ tg_status hip_fail(hipError_t e, const char *what) {
     return fail(e == hipErrorOutOfMemory ? TG_ENOMEM : TG_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
+}  // namespace
+
+namespace tg {
+// The same exits for the layer operators' files (layer_device.h).
+tg_status call_failed(tg_status st, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return st;
+}
+tg_status device_failed(hipError_t e, const char *what) { return hip_fail(e, what); }
+}  // namespace tg
+
+namespace {
+
 bool ascending_set(const int32_t *v, int32_t n) {
     if (n < 1 || n > 8) return false;
     for (int a = 0; a < n; ++a) {
