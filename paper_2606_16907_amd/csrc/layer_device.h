@@ -21,6 +21,7 @@ struct e4m3 {
 template <typename T, int N>
 using vec = T __attribute__((ext_vector_type(N)));
 using f32x4 = vec<float, 4>;
+using f32x16 = vec<float, 16>;
 using i32x4 = vec<int, 4>;
 
 // Rows may start at any element, so wide accesses are made at the element's

@@ -106,22 +106,21 @@ __device__ inline float slope(float z, int act) {
     }
 }
 
-// Four columns j .. j + 3 of row i.
-template <typename O>
-__device__ inline void finish(f32x4 z, int64_t i, int64_t j, int valid, const Epilogue &e) {
+// N columns from j on of row i.
+template <typename O, int N>
+__device__ inline void finish(vec<float, N> z, int64_t i, int64_t j, int valid, const Epilogue &e) {
     if (e.x_scale) {
-        const float sx = e.x_scale[i];
-        z *= sx;
-        z *= load_f32<float, 4>(e.w_scale + j, valid);
+        z *= e.x_scale[i];
+        z *= load_f32<float, N>(e.w_scale + j, valid);
     }
-    if (e.bias) z += load_f32<O, 4>((const O *)e.bias + j, valid);
-    if (e.pre) store_f32<O, 4>((O *)e.pre + i * e.ldp + j, z, valid);
+    if (e.bias) z += load_f32<O, N>((const O *)e.bias + j, valid);
+    if (e.pre) store_f32<O, N>((O *)e.pre + i * e.ldp + j, z, valid);
     if (e.act != TG_ACT_NONE) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) z[c] = activate(z[c], e.act);
+        for (int c = 0; c < N; ++c) z[c] = activate(z[c], e.act);
     }
-    if (e.residual) z += load_f32<O, 4>((const O *)e.residual + i * e.ldr + j, valid);
-    store_f32<O, 4>((O *)e.out + i * e.ldo + j, z, valid);
+    if (e.residual) z += load_f32<O, N>((const O *)e.residual + i * e.ldr + j, valid);
+    store_f32<O, N>((O *)e.out + i * e.ldo + j, z, valid);
 }
 
 // ---------------------------------------------------------------------------
@@ -252,14 +251,303 @@ __global__ __launch_bounds__(256) void product_any(Product a, Epilogue e, int64_
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
             const int64_t j = j0 + wj + y * 16 + (lane / 16) * 4;
-            if (j < a.nj) finish<O>(acc[x][y], i, j, (int)std::min<int64_t>(4, a.nj - j), e);
+            if (j < a.nj) finish<O, 4>(acc[x][y], i, j, (int)std::min<int64_t>(4, a.nj - j), e);
         }
     }
 }
 
+// ---------------------------------------------------------------------------
+// the product for operands whose rows start at 16-byte addresses
+// ---------------------------------------------------------------------------
+// Tiles go from memory to LDS without passing through registers; bytes past an
+// operand's end arrive as zeros, which is how rows, columns and sums that end
+// inside a tile are handled.  Two tiles a step are in LDS: while one is read the
+// next is on its way.  A step's r is multiplied in two halves, and the fragments
+// of a half are read while the half before is multiplied, across steps too, so
+// the matrix instructions wait at one barrier a step, which stands between the
+// halves: there every wave has read all of the step's tile, whose place the
+// tile after next takes, and the next tile has arrived.
+template <typename T>
+struct Wide;  // 32 x 32 matrix instructions: kDeep of them over half a step's r
+template <>
+struct Wide<bf16> {
+    static constexpr int kDeep = 2;
+    using frag = vec<bf16, 8>;
+    static __device__ f32x16 mma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Wide<f16> {
+    static constexpr int kDeep = 2;
+    using frag = vec<f16, 8>;
+    static __device__ f32x16 mma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+// The 8-bit instruction aligns groups of eight products to the largest of them
+// and drops what lies about 2^-16 below it (measured: 448 * 448 - 448 * 448 and
+// six products of 0.75 in a group give 0), then adds in 32 bits.  That is a
+// hundredth of what rounding y to 16 bits costs, and twice the speed of bf16.
+template <>
+struct Wide<e4m3> {
+    static constexpr int kDeep = 1;
+    using frag = vec<int, 8>;
+    static __device__ f32x16 mma(frag a, frag b, f32x16 c) {
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+    }
+};
+
+// Lane l's part of rows (columns) at .. at + 31, `deep` of half `half` of the step.
+template <typename T, bool kDown>
+__device__ inline typename Wide<T>::frag read_wide(const char *tile, int at, int half, int deep, int width) {
+    const int lane = threadIdx.x % 64;
+    if constexpr (sizeof(T) == 1) {
+        const int row = at + lane % 32;
+        const i32x4 lo = *(const i32x4 *)(tile + along_at(row, half * 4 + lane / 32));
+        const i32x4 hi = *(const i32x4 *)(tile + along_at(row, half * 4 + 2 + lane / 32));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else if constexpr (!kDown) {
+        return *(const typename Wide<T>::frag *)(tile + along_at(at + lane % 32, half * 4 + deep * 2 + lane / 32));
+    } else {
+        using s16x4 = vec<short, 4>;
+        using s16x8 = vec<short, 8>;
+        const int r = half * 32 + deep * 16 + (lane / 32) * 8 + (lane % 16) / 4, unit = at / 16 + (lane / 16) % 2;
+        s16x4 part[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int byte = (r + 4 * h) * width * 2 + ((unit ^ down_bits(r + 4 * h)) << 5) + (lane % 4) * 8;
+            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(tile + byte));
+        }
+        return __builtin_bit_cast(typename Wide<T>::frag, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+}
+
+// The wave's number, known to the compiler to be the same in all its lanes.
+__device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+
+// A block's share of one operand on its way to LDS: each wave moves kLoads KB a
+// tile, lane l the 16 bytes at l * 16 of each, from offsets that stay the same
+// relative to the step's first byte.
+template <typename T, bool kDown, int kWidth>
+struct Stream {
+    static constexpr int kLoads = kWidth * kStepBytes / 1024 / 4;
+    static constexpr int kRowBytes = kDown ? kWidth * 2 : kStepBytes;
+    int at[kLoads];
+    int unit;        // along: bytes of the step's r that lie before the lane's unit
+    const char *base;
+    int64_t left;    // bytes from base to the operand's end
+    int64_t step;    // bytes from one step to the next
+    int64_t r_left;  // along: bytes of r from base on
+
+    __device__ void init(const void *p, int64_t ld, int64_t at0, int64_t n_at, int64_t r0, int64_t nr, int64_t r_bytes) {
+        const int wave = wave_index(), lane = threadIdx.x % 64;
+        const int64_t row_bytes = ld * (int64_t)sizeof(T);
+        if constexpr (kDown) {
+            base = (const char *)p + r0 * row_bytes + at0 * 2;
+            // the last row may end inside a 4-byte word, which is read whole or not at all
+            left = (nr - r0 - 1) * row_bytes + ((n_at - at0) * 2 + 3) / 4 * 4;
+            step = 64 * row_bytes;
+            unit = 0;
+            r_left = 0;
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) {
+                const int place = (wave * kLoads + n) * 1024 + lane * 16, r = place / kRowBytes, b = place % kRowBytes;
+                at[n] = (int)(r * row_bytes) + ((((b >> 5) ^ down_bits(r)) << 5) | (b & 16));
+            }
+        } else {
+            base = (const char *)p + at0 * row_bytes + r0 * (int64_t)sizeof(T);
+            left = (n_at - at0 - 1) * row_bytes + r_bytes - r0 * (int64_t)sizeof(T);
+            step = kStepBytes;
+            unit = ((lane % 8) ^ (lane / 8)) * 16;
+            r_left = r_bytes - r0 * (int64_t)sizeof(T);
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) at[n] = (int)(((wave * kLoads + n) * 8 + lane / 8) * row_bytes) + unit;
+        }
+    }
+    // The step's buffer descriptor: loads past `left` give zeros.
+    __device__ i32x4 open() const {
+        const uint64_t from = (uint64_t)base;
+        i32x4 d;
+        d[0] = __builtin_amdgcn_readfirstlane((int)from);
+        d[1] = __builtin_amdgcn_readfirstlane((int)(from >> 32) & 0xffff);
+        d[2] = __builtin_amdgcn_readfirstlane((int)(left < 0 ? 0 : left > 0x7ffffff0 ? 0x7ffffff0 : left));
+        d[3] = 0x00027000;
+        return d;
+    }
+    // Starts load n of the step's tile.  As an instruction of its own, since the
+    // compiler would make every later read of LDS wait for it; the loop's waits
+    // are written out instead.  It has no output registers; m0 is the compiler's own
+    // scratch between instructions.  The pause lets m0 and a descriptor that was
+    // just written arrive.
+    __device__ void load(i32x4 d, const char *tile, int n) const {
+        const unsigned to = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)tile + (wave_index() * kLoads + n) * 1024;
+        const int off = at[n] | (!kDown && unit >= r_left ? (int)0x80000000 : 0);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :
+                     : "s"(to), "v"(off), "s"(d)
+                     : "memory");
+    }
+    __device__ void next() {
+        base += step;
+        left -= step;
+        if (!kDown) r_left -= step;
+    }
+};
+
+// Block b's tile.  Blocks go to the eight XCDs in turn, so each XCD gets a run of
+// consecutive tiles, and runs go down eight rows of tiles before they move on a
+// column: the tiles that an L2 serves at one time share rows and columns.
+__device__ inline void tile_of(int64_t b, int ti, int tj, int *i, int *j) {
+    const int total = ti * tj, share = total / 8, rest = total % 8;
+    const int xcd = (int)(b % 8), turn = (int)(b / 8);
+    const int id = xcd * share + (xcd < rest ? xcd : rest) + turn;
+    constexpr int kGroup = 8;
+    const int group = id / (kGroup * tj), in = id % (kGroup * tj);
+    const int high = ti - group * kGroup < kGroup ? ti - group * kGroup : kGroup;
+    *i = group * kGroup + in % high;
+    *j = in / high;
+}
+
+// f(kFrom), ..., f(kTo - 1) with the numbers known to the compiler.
+template <int kFrom, int kTo, typename F>
+__device__ inline void each(F f) {
+    if constexpr (kFrom < kTo) {
+        f(std::integral_constant<int, kFrom>{});
+        each<kFrom + 1, kTo>(f);
+    }
+}
+// How many of `of` things are to come before slot n of `slots`, spread evenly over
+// the first three quarters: the last have the rest to arrive.
+constexpr int share(int n, int slots, int of) {
+    const int in = slots * 3 / 4;
+    return n >= in ? of : (n * of + in - 1) / in;
+}
+
+// 64 kTI x 64 kTJ of C by four waves of 32 kTI x 32 kTJ.
+template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ>
+__global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t p_bytes) {
+    constexpr int kBI = 64 * kTI, kBJ = 64 * kTJ;
+    constexpr int kDeep = Wide<T>::kDeep;
+    constexpr int64_t kStep = kStepBytes / sizeof(T);
+    __shared__ __attribute__((aligned(1024))) char tiles[2][(kBI + kBJ) * kStepBytes];
+    using frag = typename Wide<T>::frag;
+    int bi, bj;
+    tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
+    const int64_t i0 = (int64_t)bi * kBI, j0 = (int64_t)bj * kBJ;
+    const int wave = wave_index(), lane = threadIdx.x % 64;
+    const int wi = (wave / 2) * 32 * kTI, wj = (wave % 2) * 32 * kTJ;
+
+    Stream<T, kDownP, kBI> sp;
+    Stream<T, kDownQ, kBJ> sq;
+    sp.init(a.p, a.ldp, i0, a.ni, 0, a.nr, p_bytes);
+    sq.init(a.q, a.ldq, j0, a.nj, 0, a.nr, a.nr * (int64_t)sizeof(T));
+    const auto load_all = [&](int buffer) {
+        const i32x4 dp = sp.open(), dq = sq.open();
+#pragma unroll
+        for (int n = 0; n < sp.kLoads; ++n) sp.load(dp, tiles[buffer], n);
+#pragma unroll
+        for (int n = 0; n < sq.kLoads; ++n) sq.load(dq, tiles[buffer] + kBI * kStepBytes, n);
+        sp.next();
+        sq.next();
+    };
+    f32x16 acc[kTI][kTJ] = {};
+    frag p[2][kDeep][kTI], q[2][kDeep][kTJ];
+    // Fragment f of a half, in the order of use; matrix instruction n of a half.
+    constexpr int kFrags = kDeep * (kTI + kTJ), kMma = kDeep * kTI * kTJ, kLoads = sp.kLoads + sq.kLoads;
+    const auto read = [&](int buffer, auto half, auto f) {
+        constexpr int d = f / (kTI + kTJ), n = f % (kTI + kTJ);
+        const char *const tp = tiles[buffer], *const tq = tp + kBI * kStepBytes;
+        if constexpr (n < kTJ)
+            q[half][d][n] = read_wide<T, kDownQ>(tq, wj + n * 32, half, d, kBJ);
+        else
+            p[half][d][n - kTJ] = read_wide<T, kDownP>(tp, wi + (n - kTJ) * 32, half, d, kBI);
+    };
+    const auto multiply = [&](auto half, auto n) {
+        constexpr int d = n / (kTI * kTJ), x = n / kTJ % kTI, y = n % kTJ;
+        acc[x][y] = Wide<T>::mma(q[half][d][y], p[half][d][x], acc[x][y]);
+        __builtin_amdgcn_sched_barrier(0);  // the order is as written
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+    const int steps = (int)((a.nr + kStep - 1) / kStep);
+    if (steps > 0) {
+        load_all(0);
+        load_all(1);  // past the end of r: zeros, never read
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        each<0, kFrags>([&](auto f) { read(0, first, f); });
+        for (int t = 0; t < steps; ++t) {
+            const int now = t & 1;
+            each<0, kMma>([&](auto n) {
+                each<share(n, kMma, kFrags), share(n + 1, kMma, kFrags)>([&](auto f) { read(now, second, f); });
+                multiply(first, n);
+            });
+            const i32x4 dp = sp.open(), dq = sq.open();
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            each<0, kMma>([&](auto n) {
+                each<share(n, kMma, kFrags), share(n + 1, kMma, kFrags)>([&](auto f) { read(now ^ 1, first, f); });
+                each<share(n, kMma, kLoads), share(n + 1, kMma, kLoads)>([&](auto l) {  // past the end of r, as above
+                    if constexpr (l < sp.kLoads)
+                        sp.load(dp, tiles[now], l);
+                    else
+                        sq.load(dq, tiles[now] + kBI * kStepBytes, l - sp.kLoads);
+                });
+                multiply(second, n);
+            });
+            sp.next();
+            sq.next();
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the last loads, before this LDS has another use
+    }
+    // A lane has columns 8 (c / 4) + 4 (lane / 32) + c % 4 of row lane % 32 of
+    // each 32 x 32 part.  32 rows at a time go through the wave's share of LDS, in
+    // rows 16 bytes longer than their values so that the rows of a column meet
+    // different banks, and come back 8 columns a lane, whole rows side by side.
+    __syncthreads();
+    constexpr int kRow = 32 * kTJ + 4;
+    float *const rows = (float *)&tiles[0][0] + wave * 32 * kRow;
+#pragma unroll
+    for (int x = 0; x < kTI; ++x) {
+#pragma unroll
+        for (int y = 0; y < kTJ; ++y) {
+#pragma unroll
+            for (int c = 0; c < 16; c += 4) {
+                const f32x16 v = acc[x][y];
+                *(f32x4 *)(rows + (lane % 32) * kRow + y * 32 + 2 * c + (lane / 32) * 4) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int u = lane; u < 32 * 4 * kTJ; u += 64) {
+            const int row = u / (4 * kTJ), col = u % (4 * kTJ) * 8;
+            const int64_t i = i0 + wi + x * 32 + row, j = j0 + wj + col;
+            if (i >= a.ni || j >= a.nj) continue;
+            const f32x4 lo = *(const f32x4 *)(rows + row * kRow + col), hi = *(const f32x4 *)(rows + row * kRow + col + 4);
+            finish<O, 8>(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), i, j, (int)std::min<int64_t>(8, a.nj - j), e);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Whether operand rows start at 16-byte addresses, an operand with r along its
+// rows ends on a whole unit (`r_bytes` of each row may be read), and a tile's
+// offsets fit 31 bits.
+template <typename T>
+bool streams(const void *p, int64_t ld, int64_t rows, int64_t r_bytes, bool down) {
+    const int64_t row_bytes = ld * (int64_t)sizeof(T);
+    return (uintptr_t)p % 16 == 0 && (rows < 2 || row_bytes % 16 == 0) && (down || r_bytes % 16 == 0) && row_bytes < (1 << 22);
+}
+template <typename T, bool kDownP, bool kDownQ>
+bool direct_fits(const Product &a, int64_t p_bytes) {
+    return streams<T>(a.p, a.ldp, kDownP ? a.nr : a.ni, p_bytes, kDownP) &&
+           streams<T>(a.q, a.ldq, kDownQ ? a.nr : a.nj, a.nr * (int64_t)sizeof(T), kDownQ);
+}
+
 template <typename T, typename O, bool kDownP, bool kDownQ>
-hipError_t launch_product(const Product &a, const Epilogue &e, hipStream_t s) {
+hipError_t launch_product(const Product &a, const Epilogue &e, int64_t p_bytes, hipStream_t s) {
     if (a.ni == 0 || a.nj == 0) return hipSuccess;
+    if (direct_fits<T, kDownP, kDownQ>(a, p_bytes)) {
+        const int ti = (int)ceil_div(a.ni, 256), tj = (int)ceil_div(a.nj, 256);
+        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4>), dim3(ti * tj), dim3(256), 0, s, a, e, ti, tj, p_bytes);
+        return hipGetLastError();
+    }
     const int64_t ti = ceil_div(a.ni, kAnyTile), tj = ceil_div(a.nj, kAnyTile);
     hipLaunchKernelGGL((product_any<T, O, kDownP, kDownQ>), dim3((unsigned)(ti * tj)), dim3(256), 0, s, a, e, tj);
     return hipGetLastError();
@@ -383,13 +671,13 @@ tg_status run_grad(const tg_linear_grad_args &q, const GradPlan &p, char *ws, hi
     if (q.dx) {
         Epilogue e{};
         e.out = q.dx, e.ldo = q.lddx;
-        const hipError_t r = launch_product<E, E, false, true>(Product{dz, q.w, ldz, q.ldw, q.m, q.k, q.n}, e, s);
+        const hipError_t r = launch_product<E, E, false, true>(Product{dz, q.w, ldz, q.ldw, q.m, q.k, q.n}, e, p.slope ? ldz * 2 : q.n * 2, s);
         if (r != hipSuccess) return device_failed(r, "the product dz w");
     }
     if (q.dw) {
         Epilogue e{};
         e.out = q.dw, e.ldo = q.lddw;
-        const hipError_t r = launch_product<E, E, true, true>(Product{dz, q.x, ldz, q.ldx, q.n, q.k, q.m}, e, s);
+        const hipError_t r = launch_product<E, E, true, true>(Product{dz, q.x, ldz, q.ldx, q.n, q.k, q.m}, e, 0, s);
         if (r != hipSuccess) return device_failed(r, "the product dz^T x");
     }
     return TG_OK;
@@ -433,15 +721,16 @@ tg_status tg_linear(const tg_linear_args *q, void *d_ws, size_t ws_bytes, tg_str
     const Product a{q->x, q->w, q->ldx, q->ldw, q->m, q->n, q->k};
     const Epilogue e{q->x_scale, q->w_scale, q->bias, q->residual, q->y, q->pre, q->ldr, q->ldy, q->ldp, q->act};
     const hipStream_t s = (hipStream_t)stream;
+    const int64_t x_bytes = q->k * (q->type == TG_E4M3 ? 1 : 2);
     hipError_t r;
     if (q->type == TG_BF16)
-        r = launch_product<bf16, bf16, false, false>(a, e, s);
+        r = launch_product<bf16, bf16, false, false>(a, e, x_bytes, s);
     else if (q->type == TG_F16)
-        r = launch_product<f16, f16, false, false>(a, e, s);
+        r = launch_product<f16, f16, false, false>(a, e, x_bytes, s);
     else if (q->out_type == TG_BF16)
-        r = launch_product<e4m3, bf16, false, false>(a, e, s);
+        r = launch_product<e4m3, bf16, false, false>(a, e, x_bytes, s);
     else
-        r = launch_product<e4m3, f16, false, false>(a, e, s);
+        r = launch_product<e4m3, f16, false, false>(a, e, x_bytes, s);
     return r == hipSuccess ? TG_OK : device_failed(r, "the product x w^T");
 }
 

@@ -76,6 +76,26 @@ def test_gradients(m, k, n, dtype, pad):
         R.within(got, *want[key], key)
 
 
+@pytest.mark.parametrize("m,k,n", [(129, 121, 121), (57, 249, 313), (300, 505, 65), (1, 57, 1), (3, 1, 121)])
+def test_gradients_of_odd_rows_inside_aligned_ones(m, k, n):
+    """Rows start at 16-byte addresses and end inside a 4-byte word, the operands' last ones at the buffers' ends."""
+    gen = R.generator("odd rows", m, k, n)
+
+    def rows(a, b, std=1.0):
+        ld = -(-b // 8) * 8
+        flat = (torch.randn((a - 1) * ld + b, generator=gen) * std).to(BF16).cuda()
+        return flat.as_strided((a, b), (ld, 1))
+
+    x, w, dy, pre = rows(m, k), rows(n, k, k ** -0.5), rows(m, n), rows(m, n)
+    for name in ("none", "silu"):
+        dx, dw, db = layer().tg_linear_grad(dy, x, w, pre=pre, act=name, bias_grad=True)
+        want = R.linear_grads(dy, x, w, pre, name)
+        for key, got in (("dx", dx), ("dw", dw), ("db", db)):
+            R.within(got, *want[key], key)
+        want, z, bound = R.linear(x, w, None, name)
+        R.within(layer().tg_linear(x, w, act=name), want, R.linear_bound(want, z, bound, BF16), "y")
+
+
 @pytest.mark.parametrize("name", ["relu", "silu", "gelu"])
 def test_gradients_against_differences(name):
     """Central differences of the loss sum(dy y) in 64 bits: their own error is h^2 / 6 times a third derivative (bounded by
