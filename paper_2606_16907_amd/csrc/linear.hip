@@ -19,14 +19,14 @@ namespace {
 // ---------------------------------------------------------------------------
 // A tile holds kStepBytes of r for each of its rows (or columns).  With r along
 // the rows ("along") it is [rows][128 bytes], and the 16-byte units of a row are
-// permuted by the row, unit ^ (row & 7), so that the 16 rows of a fragment meet
-// different banks.  With r down the columns ("down", 16-bit types) it is
+// permuted by the row, unit ^ (row / 2 & 7), so that 16 rows of one unit fill
+// the 64 banks once: even rows one half of them, odd rows the other.  With r down the columns ("down", 16-bit types) it is
 // [64 r][columns], read through the transposing LDS load, and the 32-byte units
 // of a row are permuted by the row's bits 0, 1 and 3, the ones in which the rows
 // of one load differ.
 constexpr int kStepBytes = 128;
 
-__device__ inline int along_at(int row, int unit) { return row * kStepBytes + ((unit ^ (row & 7)) << 4); }
+__device__ inline int along_at(int row, int unit) { return row * kStepBytes + ((unit ^ ((row >> 1) & 7)) << 4); }
 __device__ inline int down_bits(int r) { return (r & 3) | ((r >> 1) & 4); }
 
 template <typename T>
@@ -294,30 +294,49 @@ struct Wide<e4m3> {
     }
 };
 
-// Lane l's part of rows (columns) at .. at + 31, `deep` of half `half` of the step.
-template <typename T, bool kDown>
-__device__ inline typename Wide<T>::frag read_wide(const char *tile, int at, int half, int deep, int width) {
-    const int lane = threadIdx.x % 64;
-    if constexpr (sizeof(T) == 1) {
-        const int row = at + lane % 32;
-        const i32x4 lo = *(const i32x4 *)(tile + along_at(row, half * 4 + lane / 32));
-        const i32x4 hi = *(const i32x4 *)(tile + along_at(row, half * 4 + 2 + lane / 32));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else if constexpr (!kDown) {
-        return *(const typename Wide<T>::frag *)(tile + along_at(at + lane % 32, half * 4 + deep * 2 + lane / 32));
-    } else {
-        using s16x4 = vec<short, 4>;
-        using s16x8 = vec<short, 8>;
-        const int r = half * 32 + deep * 16 + (lane / 32) * 8 + (lane % 16) / 4, unit = at / 16 + (lane / 16) % 2;
-        s16x4 part[2];
+// Where a lane reads its parts of an operand's tile.  A part's byte is a lane's
+// own offset, of which there are four (the wave's rows or columns begin at a
+// multiple of 64, so the permutations leave the rest alone), plus a number the
+// compiler knows: the reads need no arithmetic.
+template <typename T, bool kDown, int kWidth>
+struct Reader {
+    using frag = typename Wide<T>::frag;
+    int lane_at[4];
+    // The wave's rows (columns) begin at w0.
+    __device__ void init(int w0) {
+        const int lane = threadIdx.x % 64;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int byte = (r + 4 * h) * width * 2 + ((unit ^ down_bits(r + 4 * h)) << 5) + (lane % 4) * 8;
-            part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(tile + byte));
+        for (int c = 0; c < 4; ++c) {
+            if constexpr (kDown) {  // by the 32 columns; rows of r are constants
+                const int r = (lane / 32) * 8 + (lane % 16) / 4;
+                lane_at[c] = r * kWidth * 2 + (((w0 / 16 + 2 * c + (lane / 16) % 2) ^ down_bits(r)) << 5) + (lane % 4) * 8;
+            } else {  // by the pair of units
+                lane_at[c] = along_at(w0 + lane % 32, 2 * c + lane / 32);
+            }
         }
-        return __builtin_bit_cast(typename Wide<T>::frag, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
-}
+    // Rows (columns) 32 n .. 32 n + 31 of the wave, instruction d of half `half`.
+    template <int half, int d, int n>
+    __device__ frag read(const char *tile) const {
+        if constexpr (sizeof(T) == 1) {
+            const i32x4 lo = *(const i32x4 *)(tile + lane_at[half * 2] + n * 32 * kStepBytes);
+            const i32x4 hi = *(const i32x4 *)(tile + lane_at[half * 2 + 1] + n * 32 * kStepBytes);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else if constexpr (!kDown) {
+            return *(const frag *)(tile + lane_at[half * 2 + d] + n * 32 * kStepBytes);
+        } else {
+            using s16x4 = vec<short, 4>;
+            using s16x8 = vec<short, 8>;
+            s16x4 part[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {  // rows of r 4 on: bit 2, which the permutation does not see
+                const char *const from = tile + lane_at[n] + (half * 32 + d * 16 + 4 * h) * kWidth * 2;
+                part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
+            }
+            return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
 
 // The wave's number, known to the compiler to be the same in all its lanes.
 __device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
@@ -330,7 +349,7 @@ struct Stream {
     static constexpr int kLoads = kWidth * kStepBytes / 1024 / 4;
     static constexpr int kRowBytes = kDown ? kWidth * 2 : kStepBytes;
     int at[kLoads];
-    int unit;        // along: bytes of the step's r that lie before the lane's unit
+    int unit;        // along: bytes of the step's r before the lane's unit, in even loads; odd ones are half a row on
     const char *base;
     int64_t left;    // bytes from base to the operand's end
     int64_t step;    // bytes from one step to the next
@@ -355,14 +374,21 @@ struct Stream {
             base = (const char *)p + at0 * row_bytes + r0 * (int64_t)sizeof(T);
             left = (n_at - at0 - 1) * row_bytes + r_bytes - r0 * (int64_t)sizeof(T);
             step = kStepBytes;
-            unit = ((lane % 8) ^ (lane / 8)) * 16;
+            unit = ((lane % 8) ^ (lane / 16)) * 16;
             r_left = r_bytes - r0 * (int64_t)sizeof(T);
 #pragma unroll
-            for (int n = 0; n < kLoads; ++n) at[n] = (int)(((wave * kLoads + n) * 8 + lane / 8) * row_bytes) + unit;
+            for (int n = 0; n < kLoads; ++n) at[n] = (int)(((wave * kLoads + n) * 8 + lane / 8) * row_bytes) + (unit ^ n % 2 * 64);
         }
     }
-    // The step's buffer descriptor: loads past `left` give zeros.
-    __device__ i32x4 open() const {
+    // The step's buffer descriptor: loads past `left` give zeros, and so do
+    // offsets of 2^31 and more, which the lanes get whose unit lies past the row's
+    // end (they stay there: later steps lie past it as a whole).
+    __device__ i32x4 open() {
+        if (!kDown) {
+            const int outside[2] = {unit >= r_left ? (int)0x80000000 : 0, (unit ^ 64) >= r_left ? (int)0x80000000 : 0};
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) at[n] |= outside[n % 2];
+        }
         const uint64_t from = (uint64_t)base;
         i32x4 d;
         d[0] = __builtin_amdgcn_readfirstlane((int)from);
@@ -371,18 +397,16 @@ struct Stream {
         d[3] = 0x00027000;
         return d;
     }
-    // Starts load n of the step's tile.  As an instruction of its own, since the
-    // compiler would make every later read of LDS wait for it; the loop's waits
-    // are written out instead.  It has no output registers; m0 is the compiler's own
-    // scratch between instructions.  The pause lets m0 and a descriptor that was
-    // just written arrive.
-    __device__ void load(i32x4 d, const char *tile, int n) const {
-        const unsigned to = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char *)tile + (wave_index() * kLoads + n) * 1024;
-        const int off = at[n] | (!kDown && unit >= r_left ? (int)0x80000000 : 0);
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+    // Starts load n of the step's tile, `tile` bytes into LDS.  As an instruction of
+    // its own, since the compiler would make every later read of LDS wait for it;
+    // the loop's waits are written out instead.  It has no output registers.  The
+    // pause is for m0, which belongs to no one between instructions.
+    template <int n>
+    __device__ void load(i32x4 d, unsigned tile) const {
+        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                      :
-                     : "s"(to), "v"(off), "s"(d)
-                     : "memory");
+                     : "s"(tile), "v"(at[n]), "s"(d), "n"(n * 1024)
+                     : "memory", "scc");
     }
     __device__ void next() {
         base += step;
@@ -413,12 +437,8 @@ __device__ inline void each(F f) {
         each<kFrom + 1, kTo>(f);
     }
 }
-// How many of `of` things are to come before slot n of `slots`, spread evenly over
-// the first three quarters: the last have the rest to arrive.
-constexpr int share(int n, int slots, int of) {
-    const int in = slots * 3 / 4;
-    return n >= in ? of : (n * of + in - 1) / in;
-}
+// How many of `of` things are to come before slot n, spread evenly over `slots`.
+constexpr int share(int n, int slots, int of) { return n >= slots ? of : (n * of + slots - 1) / slots; }
 
 // 64 kTI x 64 kTJ of C by four waves of 32 kTI x 32 kTJ.
 template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ>
@@ -426,7 +446,8 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     constexpr int kBI = 64 * kTI, kBJ = 64 * kTJ;
     constexpr int kDeep = Wide<T>::kDeep;
     constexpr int64_t kStep = kStepBytes / sizeof(T);
-    __shared__ __attribute__((aligned(1024))) char tiles[2][(kBI + kBJ) * kStepBytes];
+    constexpr int kTileP = kBI * kStepBytes, kTile = kTileP + kBJ * kStepBytes;
+    __shared__ __attribute__((aligned(1024))) char tiles[2][kTile];
     using frag = typename Wide<T>::frag;
     int bi, bj;
     tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
@@ -436,28 +457,30 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
 
     Stream<T, kDownP, kBI> sp;
     Stream<T, kDownQ, kBJ> sq;
+    Reader<T, kDownP, kBI> rp;
+    Reader<T, kDownQ, kBJ> rq;
     sp.init(a.p, a.ldp, i0, a.ni, 0, a.nr, p_bytes);
     sq.init(a.q, a.ldq, j0, a.nj, 0, a.nr, a.nr * (int64_t)sizeof(T));
-    const auto load_all = [&](int buffer) {
-        const i32x4 dp = sp.open(), dq = sq.open();
-#pragma unroll
-        for (int n = 0; n < sp.kLoads; ++n) sp.load(dp, tiles[buffer], n);
-#pragma unroll
-        for (int n = 0; n < sq.kLoads; ++n) sq.load(dq, tiles[buffer] + kBI * kStepBytes, n);
-        sp.next();
-        sq.next();
-    };
+    rp.init(wi);
+    rq.init(wj);
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&tiles[0][0];
+    const unsigned to_p = lds + wave * sp.kLoads * 1024, to_q = lds + kTileP + wave * sq.kLoads * 1024;
     f32x16 acc[kTI][kTJ] = {};
     frag p[2][kDeep][kTI], q[2][kDeep][kTJ];
-    // Fragment f of a half, in the order of use; matrix instruction n of a half.
-    constexpr int kFrags = kDeep * (kTI + kTJ), kMma = kDeep * kTI * kTJ, kLoads = sp.kLoads + sq.kLoads;
-    const auto read = [&](int buffer, auto half, auto f) {
-        constexpr int d = f / (kTI + kTJ), n = f % (kTI + kTJ);
-        const char *const tp = tiles[buffer], *const tq = tp + kBI * kStepBytes;
-        if constexpr (n < kTJ)
-            q[half][d][n] = read_wide<T, kDownQ>(tq, wj + n * 32, half, d, kBJ);
+    // Load l, fragment f and matrix instruction n, each in the order of use.
+    constexpr int kLoads = sp.kLoads + sq.kLoads, kFrags = kDeep * (kTI + kTJ), kMma = kDeep * kTI * kTJ;
+    const auto load = [&](auto buffer, i32x4 dp, i32x4 dq, auto l) {
+        if constexpr (l < sp.kLoads)
+            sp.template load<l>(dp, to_p + buffer * kTile);
         else
-            p[half][d][n - kTJ] = read_wide<T, kDownP>(tp, wi + (n - kTJ) * 32, half, d, kBI);
+            sq.template load<l - sp.kLoads>(dq, to_q + buffer * kTile);
+    };
+    const auto read = [&](auto buffer, auto half, auto f) {
+        constexpr int d = f / (kTI + kTJ), n = f % (kTI + kTJ);
+        if constexpr (n < kTJ)
+            q[half][d][n] = rq.template read<half, d, n>(&tiles[buffer][kTileP]);
+        else
+            p[half][d][n - kTJ] = rp.template read<half, d, n - kTJ>(&tiles[buffer][0]);
     };
     const auto multiply = [&](auto half, auto n) {
         constexpr int d = n / (kTI * kTJ), x = n / kTJ % kTI, y = n % kTJ;
@@ -466,33 +489,46 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     };
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
+    // The barrier comes before the last kTail instructions of the first half, so
+    // that they keep the matrix unit busy while the waves meet; a slot is the gap
+    // before a matrix instruction, and little may stand in it: there is one wave to
+    // a SIMD, an instruction takes it some 4 cycles, a matrix instruction 32.
+    constexpr int kTail = kMma / 8, kReadSlots = kMma * 5 / 8, kLoadSlots = kMma * 3 / 4;
+    i32x4 dp, dq;
+    const auto step = [&](auto now) {
+        constexpr std::integral_constant<int, 1 - now> other{};
+        each<0, kMma - kTail>([&](auto n) {
+            each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(now, second, f); });
+            if constexpr (n == kReadSlots) dp = sp.open();
+            if constexpr (n == kReadSlots + 1) dq = sq.open();
+            if constexpr (n == kReadSlots + 2) sp.next(), sq.next();
+            multiply(first, n);
+        });
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        each<kMma - kTail, kMma>([&](auto n) {
+            each<share(n - kMma + kTail, kLoadSlots, kLoads), share(n - kMma + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, dp, dq, l); });
+            multiply(first, n);
+        });
+        each<0, kMma>([&](auto n) {
+            each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(other, first, f); });
+            each<share(n + kTail, kLoadSlots, kLoads), share(n + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, dp, dq, l); });
+            multiply(second, n);
+        });
+    };
+    // loads past the end of r give zeros, so two steps at a time are right for any number
     const int steps = (int)((a.nr + kStep - 1) / kStep);
     if (steps > 0) {
-        load_all(0);
-        load_all(1);  // past the end of r: zeros, never read
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        each<0, kFrags>([&](auto f) { read(0, first, f); });
-        for (int t = 0; t < steps; ++t) {
-            const int now = t & 1;
-            each<0, kMma>([&](auto n) {
-                each<share(n, kMma, kFrags), share(n + 1, kMma, kFrags)>([&](auto f) { read(now, second, f); });
-                multiply(first, n);
-            });
-            const i32x4 dp = sp.open(), dq = sq.open();
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            each<0, kMma>([&](auto n) {
-                each<share(n, kMma, kFrags), share(n + 1, kMma, kFrags)>([&](auto f) { read(now ^ 1, first, f); });
-                each<share(n, kMma, kLoads), share(n + 1, kMma, kLoads)>([&](auto l) {  // past the end of r, as above
-                    if constexpr (l < sp.kLoads)
-                        sp.load(dp, tiles[now], l);
-                    else
-                        sq.load(dq, tiles[now] + kBI * kStepBytes, l - sp.kLoads);
-                });
-                multiply(second, n);
-            });
-            sp.next();
-            sq.next();
+        each<0, 2>([&](auto buffer) {
+            dp = sp.open(), dq = sq.open();
+            asm volatile("s_nop 4" ::: "memory");  // a descriptor just written may not be read at once
+            each<0, kLoads>([&](auto l) { load(buffer, dp, dq, l); });
+            sp.next(), sq.next();
+        });
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        each<0, kFrags>([&](auto f) { read(first, first, f); });
+        for (int t = 0; t < steps; t += 2) {
+            step(first);
+            step(second);
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the last loads, before this LDS has another use
     }
