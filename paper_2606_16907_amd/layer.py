@@ -76,10 +76,14 @@ def load_library():
     return L
 
 
+def _elsewhere(t, what, device):
+    return ValueError(f"{what}: on {t.device}, the current device cuda:{device} expected")
+
+
 def _matrix(t, dtype, rows, cols, what, device):
     """Pointer and row stride of a [rows, cols] matrix; any None size is the tensor's own."""
-    if not t.is_cuda or t.device.index != device:
-        raise ValueError(f"{what}: on {t.device}, cuda:{device} expected")
+    if t.get_device() != device:
+        raise _elsewhere(t, what, device)
     if t.dtype != dtype:
         raise ValueError(f"{what}: dtype {t.dtype}, {dtype} expected")
     if t.dim() != 2:
@@ -96,8 +100,8 @@ def _matrix(t, dtype, rows, cols, what, device):
 
 
 def _vector(t, dtype, n, what, device):
-    if not t.is_cuda or t.device.index != device:
-        raise ValueError(f"{what}: on {t.device}, cuda:{device} expected")
+    if t.get_device() != device:
+        raise _elsewhere(t, what, device)
     if t.dtype != dtype:
         raise ValueError(f"{what}: dtype {t.dtype}, {dtype} expected")
     if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
@@ -105,27 +109,20 @@ def _vector(t, dtype, n, what, device):
     return t.data_ptr()
 
 
-def _device(t, what):
-    """The index of the current device, which the first operand has to be on."""
-    device = torch.cuda.current_device()
-    if not t.is_cuda or t.device.index != device:
-        raise ValueError(f"{what}: on {t.device}, the current device cuda:{device} expected")
-    return device
+# torch.cuda.current_stream(device).cuda_stream without the Stream object around it
+# (0.1 us in place of 1.2; a call of the smallest kernels takes 10 in all)
+_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-def _workspace(bytes_, given, what, device):
+def _workspace(size, given, like, device):
+    """Pointer and size of the given workspace or of a new one, and what keeps it
+    until the call is queued: the allocator hands it out again on this stream only."""
     if given is not None:
-        p, n = T._dws(given, what, device)
-        return p, n
-    if not bytes_:
-        return None, 0
-    # freed on return: the allocator hands it out again on this stream only
-    t = torch.empty(bytes_, dtype=torch.uint8, device=f"cuda:{device}")
-    return t.data_ptr(), bytes_
+        return (*T._dws(given, "workspace", device), given)
+    if not size:
+        return None, 0, None
+    t = like.new_empty(size, dtype=torch.uint8)
+    return t.data_ptr(), size, t
 
 
 def _act(act):
@@ -134,10 +131,12 @@ def _act(act):
     return ACTS[act]
 
 
-def _out(out, shape, dtype, device, what):
+def _out(out, like, m, n, dtype, device):
+    """The [m, n] output, its pointer and row stride."""
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=f"cuda:{device}")
-    return out, *_matrix(out, dtype, *shape, what, device)
+        out = like.new_empty((m, n), dtype=dtype)
+        return out, out.data_ptr(), n
+    return out, *_matrix(out, dtype, m, n, "out", device)
 
 
 def tg_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=None, out_dtype=None,
@@ -149,7 +148,7 @@ def tg_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=
     holds x w^T + bias, None without an activation: what tg_linear_grad wants.
     `out` receives y and may be the residual."""
     lib = load_library()
-    device = _device(x, "x")
+    device = torch.cuda.current_device()
     dtype = x.dtype
     if dtype not in TYPES or dtype == torch.float32:
         raise ValueError(f"x: dtype {dtype}, bfloat16, float16 or float8_e4m3fn expected")
@@ -168,11 +167,11 @@ def tg_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=
     pb = None if bias is None else _vector(bias, out_dtype, n, "bias", device)
     pr, ldr = (None, 0) if residual is None else _matrix(residual, out_dtype, m, n, "residual", device)
     act = _act(act)
-    y, py, ldy = _out(out, (m, n), out_dtype, device, "out")
-    pre, pp, ldp = _out(None, (m, n), out_dtype, device, "pre") if keep_pre and act else (None, None, 0)
+    y, py, ldy = _out(out, x, m, n, out_dtype, device)
+    pre, pp, ldp = _out(None, x, m, n, out_dtype, device) if keep_pre and act else (None, None, 0)
     a = TgLinearArgs(px, pw, psx, psw, pb, pr, py, pp, m, n, k, ldx, ldw, ldr, ldy, ldp, TYPES[dtype],
                      TYPES[out_dtype], act, 0)
-    ws, size = _workspace(lib.tg_linear_workspace_bytes(a), workspace, "workspace", device)
+    ws, size, _kept = _workspace(lib.tg_linear_workspace_bytes(a), workspace, x, device)
     T._check(lib.tg_linear(a, ws, size, _stream(device)), "tg_linear")
     return (y, pre) if keep_pre else y
 
@@ -182,7 +181,7 @@ def tg_linear_grad(dy, x, w, pre=None, act="none", bias_grad=False, x_grad=True,
     not asked for are None.  The residual's gradient is dy.  `pre` is
     tg_linear's, needed where there is an activation."""
     lib = load_library()
-    device = _device(dy, "dy")
+    device = torch.cuda.current_device()
     dtype = dy.dtype
     if dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"dy: dtype {dtype}, bfloat16 or float16 expected")
@@ -195,12 +194,12 @@ def tg_linear_grad(dy, x, w, pre=None, act="none", bias_grad=False, x_grad=True,
     if act and pre is None:
         raise ValueError("pre: needed for the gradient of an activation (tg_linear with keep_pre)")
     pp, ldp = _matrix(pre, dtype, m, n, "pre", device) if act else (None, 0)
-    dx, pdx, lddx = _out(None, (m, k), dtype, device, "dx") if x_grad else (None, None, 0)
-    dw, pdw, lddw = _out(None, (n, k), dtype, device, "dw") if w_grad else (None, None, 0)
-    db = torch.empty(n, dtype=dtype, device=dy.device) if bias_grad else None
+    dx, pdx, lddx = _out(None, dy, m, k, dtype, device) if x_grad else (None, None, 0)
+    dw, pdw, lddw = _out(None, dy, n, k, dtype, device) if w_grad else (None, None, 0)
+    db = dy.new_empty(n) if bias_grad else None
     a = TgLinearGradArgs(pdy, pp, px, pw, pdx, pdw, None if db is None else db.data_ptr(), m, n, k, lddy, ldp, ldx, ldw,
                          lddx, lddw, TYPES[dtype], act)
-    ws, size = _workspace(lib.tg_linear_grad_workspace_bytes(a), workspace, "workspace", device)
+    ws, size, _kept = _workspace(lib.tg_linear_grad_workspace_bytes(a), workspace, dy, device)
     T._check(lib.tg_linear_grad(a, ws, size, _stream(device)), "tg_linear_grad")
     return dx, dw, db
 
@@ -209,15 +208,16 @@ class Norm(NamedTuple):
     y: torch.Tensor
     scale: Optional[torch.Tensor]  # [rows], 8-bit outputs only
     hidden: torch.Tensor           # x + residual; x itself where there is no residual
-    rstd: torch.Tensor             # [rows]
+    rstd: Optional[torch.Tensor]   # [rows], for the gradient
 
 
-def tg_rms_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, out=None):
+def tg_rms_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, out=None, keep_rstd=None):
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight over rows of
     float32, bfloat16 or float16; with out_dtype float8_e4m3fn y is y / scale
-    for a scale per row."""
+    for a scale per row.  rstd, which the gradient takes, is returned with
+    outputs in the inputs' type, or as keep_rstd says."""
     lib = load_library()
-    device = _device(x, "x")
+    device = torch.cuda.current_device()
     dtype = x.dtype
     if dtype not in TYPES or dtype == E4M3:
         raise ValueError(f"x: dtype {dtype}, float32, bfloat16 or float16 expected")
@@ -229,12 +229,14 @@ def tg_rms_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, out=None):
     rows, cols = x.shape
     pw = _vector(weight, dtype, cols, "weight", device)
     pr, ldr = (None, 0) if residual is None else _matrix(residual, dtype, rows, cols, "residual", device)
-    hidden, ph, ldh = (x, None, 0) if residual is None else _out(None, (rows, cols), dtype, device, "hidden")
-    y, py, ldy = _out(out, (rows, cols), out_dtype, device, "out")
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device) if out_dtype == E4M3 else None
-    a = TgRmsNormArgs(px, pr, pw, ph, py, None if scale is None else scale.data_ptr(), rstd.data_ptr(), rows, cols,
-                      ldx, ldr, ldh, ldy, eps, TYPES[dtype], TYPES[out_dtype], 0)
+    eight = out_dtype == E4M3
+    hidden, ph, ldh = (x, None, 0) if residual is None else _out(None, x, rows, cols, dtype, device)
+    y, py, ldy = _out(out, x, rows, cols, out_dtype, device)
+    scale = x.new_empty(rows, dtype=torch.float32) if eight else None
+    rstd = x.new_empty(rows, dtype=torch.float32) if keep_rstd or (keep_rstd is None and not eight) else None
+    a = TgRmsNormArgs(px, pr, pw, ph, py, None if scale is None else scale.data_ptr(),
+                      None if rstd is None else rstd.data_ptr(), rows, cols, ldx, ldr, ldh, ldy, eps, TYPES[dtype],
+                      TYPES[out_dtype], 0)
     T._check(lib.tg_rms_norm(a, _stream(device)), "tg_rms_norm")
     return Norm(y, scale, hidden, rstd)
 
@@ -243,7 +245,7 @@ def tg_rms_norm_grad(dy, hidden, weight, rstd, dhidden=None, workspace=None):
     """(dx, dweight) of tg_rms_norm; dx is the gradient of x and of the residual
     alike.  dhidden is the gradient that arrives at `hidden` from further on."""
     lib = load_library()
-    device = _device(dy, "dy")
+    device = torch.cuda.current_device()
     dtype = dy.dtype
     if dtype not in TYPES or dtype == E4M3:
         raise ValueError(f"dy: dtype {dtype}, float32, bfloat16 or float16 expected")
@@ -253,11 +255,11 @@ def tg_rms_norm_grad(dy, hidden, weight, rstd, dhidden=None, workspace=None):
     pw = _vector(weight, dtype, cols, "weight", device)
     ps = _vector(rstd, torch.float32, rows, "rstd", device)
     pdh, lddh = (None, 0) if dhidden is None else _matrix(dhidden, dtype, rows, cols, "dhidden", device)
-    dx, pdx, lddx = _out(None, (rows, cols), dtype, device, "dx")
-    dweight = torch.empty(cols, dtype=dtype, device=dy.device)
+    dx, pdx, lddx = _out(None, dy, rows, cols, dtype, device)
+    dweight = dy.new_empty(cols)
     a = TgRmsNormGradArgs(pdy, pdh, ph, pw, ps, pdx, dweight.data_ptr(), rows, cols, lddy, lddh, ldh, lddx,
                           TYPES[dtype], 0)
-    ws, size = _workspace(lib.tg_rms_norm_grad_workspace_bytes(a), workspace, "workspace", device)
+    ws, size, _kept = _workspace(lib.tg_rms_norm_grad_workspace_bytes(a), workspace, dy, device)
     T._check(lib.tg_rms_norm_grad(a, ws, size, _stream(device)), "tg_rms_norm_grad")
     return dx, dweight
 
@@ -326,8 +328,8 @@ class AdamW:
                 n = params[i].numel()
                 if name.endswith("scale"):
                     n = -(-n // SCALE_BLOCK)
-                if not t.is_cuda or t.device.index != self.device:
-                    raise ValueError(f"{name} {i}: on {t.device}, the current device cuda:{self.device} expected")
+                if t.get_device() != self.device:
+                    raise _elsewhere(t, f"{name} {i}", self.device)
                 if t.dtype != want[name]:
                     raise ValueError(f"{name} {i}: dtype {t.dtype}, {want[name]} expected")
                 if not t.is_contiguous() or t.numel() != n:
