@@ -325,36 +325,39 @@ struct Wide<e4m3> {
 template <typename T, bool kDown, int kWidth>
 struct Reader {
     using frag = typename Wide<T>::frag;
-    int lane_at[4];
-    // The wave's rows (columns) begin at w0.
-    __device__ void init(int w0) {
+    int lane_at[2][4];  // by buffer: constants reach 2^16 bytes
+    // The wave's rows (columns) begin at w0; the operand's tile `begin` bytes into a
+    // buffer, and a buffer `size` bytes after the one before.
+    __device__ void init(int w0, int begin, int size) {
         const int lane = threadIdx.x % 64;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             if constexpr (kDown) {  // by the 32 columns; rows of r are constants
                 const int r = (lane / 32) * 8 + (lane % 16) / 4;
-                lane_at[c] = r * kWidth * 2 + (((w0 / 16 + 2 * c + (lane / 16) % 2) ^ down_bits(r)) << 5) + (lane % 4) * 8;
+                lane_at[0][c] = begin + r * kWidth * 2 + (((w0 / 16 + 2 * c + (lane / 16) % 2) ^ down_bits(r)) << 5) + (lane % 4) * 8;
             } else {  // by the pair of units
-                lane_at[c] = along_at(w0 + lane % 32, 2 * c + lane / 32);
+                lane_at[0][c] = begin + along_at(w0 + lane % 32, 2 * c + lane / 32);
             }
+            lane_at[1][c] = lane_at[0][c] + size;
+            asm volatile("" : "+v"(lane_at[1][c]));  // a register of its own, not an addition at every read
         }
     }
     // Rows (columns) 32 n .. 32 n + 31 of the wave, instruction d of half `half`.
-    template <int half, int d, int n>
-    __device__ frag read(const char *tile) const {
+    template <int buffer, int half, int d, int n>
+    __device__ frag read(const char *lds) const {
         if constexpr (sizeof(T) == 1) {
-            const i32x4 lo = *(const i32x4 *)(tile + lane_at[half * 2] + n * 32 * kStepBytes);
-            const i32x4 hi = *(const i32x4 *)(tile + lane_at[half * 2 + 1] + n * 32 * kStepBytes);
+            const i32x4 lo = *(const i32x4 *)(lds + lane_at[buffer][half * 2] + n * 32 * kStepBytes);
+            const i32x4 hi = *(const i32x4 *)(lds + lane_at[buffer][half * 2 + 1] + n * 32 * kStepBytes);
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         } else if constexpr (!kDown) {
-            return *(const frag *)(tile + lane_at[half * 2 + d] + n * 32 * kStepBytes);
+            return *(const frag *)(lds + lane_at[buffer][half * 2 + d] + n * 32 * kStepBytes);
         } else {
             using s16x4 = vec<short, 4>;
             using s16x8 = vec<short, 8>;
             s16x4 part[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // rows of r 4 on: bit 2, which the permutation does not see
-                const char *const from = tile + lane_at[n] + (half * 32 + d * 16 + 4 * h) * kWidth * 2;
+                const char *const from = lds + lane_at[buffer][n] + (half * 32 + d * 16 + 4 * h) * kWidth * 2;
                 part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
             }
             return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
@@ -371,10 +374,11 @@ struct Stream {
     static constexpr int kRowBytes = kDown ? kWidth * 2 : kStepBytes;
     int at[kLoads];
     int unit;        // along: bytes of the step's r before the lane's unit, in even loads; odd ones are half a row on
-    const char *base;
-    int64_t left;    // bytes from base to the operand's end
-    int64_t step;    // bytes from one step to the next
-    int64_t r_left;  // along: bytes of r from base on
+    const char *base;      // of step 0
+    int64_t left;          // bytes from there to the operand's end
+    int64_t step;          // bytes from one step to the next
+    int64_t r_bytes_left;  // along: bytes of r from there on
+    i32x4 d;               // the step's buffer descriptor
 
     __device__ void init(const void *p, int64_t ld, int64_t at0, int64_t n_at, int64_t r0, int64_t nr, int64_t r_bytes) {
         const int wave = wave_index(), lane = threadIdx.x % 64;
@@ -385,7 +389,7 @@ struct Stream {
             left = (nr - r0 - 1) * row_bytes + ((n_at - at0) * 2 + 3) / 4 * 4;
             step = 64 * row_bytes;
             unit = 0;
-            r_left = 0;
+            r_bytes_left = 0;
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
                 const int place = (wave * kLoads + n) * 1024 + lane * 16, r = place / kRowBytes, b = place % kRowBytes;
@@ -396,43 +400,47 @@ struct Stream {
             left = (n_at - at0 - 1) * row_bytes + r_bytes - r0 * (int64_t)sizeof(T);
             step = kStepBytes;
             unit = ((lane % 8) ^ (lane / 16)) * 16;
-            r_left = r_bytes - r0 * (int64_t)sizeof(T);
+            r_bytes_left = r_bytes - r0 * (int64_t)sizeof(T);
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) at[n] = (int)(((wave * kLoads + n) * 8 + lane / 8) * row_bytes) + (unit ^ n % 2 * 64);
         }
     }
-    // The step's buffer descriptor: loads past `left` give zeros, and so do
-    // offsets of 2^31 and more, which the lanes get whose unit lies past the row's
-    // end (they stay there: later steps lie past it as a whole).
-    __device__ i32x4 open() {
+    // The buffer descriptor of step h: loads past the operand's end give zeros, and
+    // so do offsets of 2^31 and more, which the lanes get whose unit lies past the
+    // row's end (and keep: later steps lie past it as a whole).
+    __device__ void open(int h) {
+        const int64_t left_h = left - h * step;
         if (!kDown) {
+            const int64_t r_left = r_bytes_left - h * step;
             const int outside[2] = {unit >= r_left ? (int)0x80000000 : 0, (unit ^ 64) >= r_left ? (int)0x80000000 : 0};
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) at[n] |= outside[n % 2];
         }
-        const uint64_t from = (uint64_t)base;
-        i32x4 d;
+        const uint64_t from = (uint64_t)base + h * step;
         d[0] = __builtin_amdgcn_readfirstlane((int)from);
         d[1] = __builtin_amdgcn_readfirstlane((int)(from >> 32) & 0xffff);
-        d[2] = __builtin_amdgcn_readfirstlane((int)(left < 0 ? 0 : left > 0x7ffffff0 ? 0x7ffffff0 : left));
+        d[2] = __builtin_amdgcn_readfirstlane((int)(left_h < 0 ? 0 : left_h > 0x7ffffff0 ? 0x7ffffff0 : left_h));
         d[3] = 0x00027000;
-        return d;
+    }
+    // The next step's, while two whole steps at least follow it: no row and no unit
+    // ends in it that did not end before, so only the address moves.  Rows past the
+    // last (along) begin past the first step's end too; columns past the last
+    // (down) are the beginnings of rows that exist.
+    __device__ void advance() {
+        const uint64_t from = ((uint64_t)(unsigned)d[1] << 32 | (unsigned)d[0]) + (uint64_t)step;
+        d[0] = (int)from;
+        d[1] = (int)(from >> 32);
     }
     // Starts load n of the step's tile, `tile` bytes into LDS.  As an instruction of
     // its own, since the compiler would make every later read of LDS wait for it;
     // the loop's waits are written out instead.  It has no output registers.  The
     // pause is for m0, which belongs to no one between instructions.
     template <int n>
-    __device__ void load(i32x4 d, unsigned tile) const {
+    __device__ void load(unsigned tile) const {
         asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                      :
                      : "s"(tile), "v"(at[n]), "s"(d), "n"(n * 1024)
                      : "memory", "scc");
-    }
-    __device__ void next() {
-        base += step;
-        left -= step;
-        if (!kDown) r_left -= step;
     }
 };
 
@@ -485,26 +493,26 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     const int64_t r0 = (int64_t)blockIdx.y * share_steps * kStep, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kStep);
     sp.init(a.p, a.ldp, i0, a.ni, r0, r1, r1 < a.nr ? r1 * (int64_t)sizeof(T) : p_bytes);
     sq.init(a.q, a.ldq, j0, a.nj, r0, r1, r1 * (int64_t)sizeof(T));
-    rp.init(wi);
-    rq.init(wj);
+    rp.init(wi, 0, kTile);
+    rq.init(wj, kTileP, kTile);
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&tiles[0][0];
     const unsigned to_p = lds + wave * sp.kLoads * 1024, to_q = lds + kTileP + wave * sq.kLoads * 1024;
     f32x16 acc[kTI][kTJ] = {};
     frag p[2][kDeep][kTI], q[2][kDeep][kTJ];
     // Load l, fragment f and matrix instruction n, each in the order of use.
     constexpr int kLoads = sp.kLoads + sq.kLoads, kFrags = kDeep * (kTI + kTJ), kMma = kDeep * kTI * kTJ;
-    const auto load = [&](auto buffer, i32x4 dp, i32x4 dq, auto l) {
+    const auto load = [&](auto buffer, auto l) {
         if constexpr (l < sp.kLoads)
-            sp.template load<l>(dp, to_p + buffer * kTile);
+            sp.template load<l>(to_p + buffer * kTile);
         else
-            sq.template load<l - sp.kLoads>(dq, to_q + buffer * kTile);
+            sq.template load<l - sp.kLoads>(to_q + buffer * kTile);
     };
     const auto read = [&](auto buffer, auto half, auto f) {
         constexpr int d = f / (kTI + kTJ), n = f % (kTI + kTJ);
         if constexpr (n < kTJ)
-            q[half][d][n] = rq.template read<half, d, n>(&tiles[buffer][kTileP]);
+            q[half][d][n] = rq.template read<buffer, half, d, n>(&tiles[0][0]);
         else
-            p[half][d][n - kTJ] = rp.template read<half, d, n - kTJ>(&tiles[buffer][0]);
+            p[half][d][n - kTJ] = rp.template read<buffer, half, d, n - kTJ>(&tiles[0][0]);
     };
     const auto multiply = [&](auto half, auto n) {
         constexpr int d = n / (kTI * kTJ), x = n / kTJ % kTI, y = n % kTJ;
@@ -519,40 +527,44 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     // a SIMD, an instruction takes it some 4 cycles, a matrix instruction 32.
     constexpr int kTail = kMma / 8, kReadSlots = kMma * 5 / 8, kLoadSlots = kMma * 3 / 4;
     static_assert(kReadSlots + 2 <= kMma - kTail, "the descriptors are made between the reads and the barrier");
-    i32x4 dp, dq;
-    const auto step = [&](auto now) {
+    // Step t, from buffer `now`; `inner`: step t + 2 is one that advance() may reach.
+    const auto step = [&](auto now, auto inner, int t) {
         constexpr std::integral_constant<int, 1 - now> other{};
         each<0, kMma - kTail>([&](auto n) {
             each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(now, second, f); });
-            if constexpr (n == kReadSlots) dp = sp.open();
-            if constexpr (n == kReadSlots + 1) dq = sq.open(), sp.next(), sq.next();
+            if constexpr (n == kReadSlots) inner ? sp.advance() : sp.open(t + 2);
+            if constexpr (n == kReadSlots + 1) inner ? sq.advance() : sq.open(t + 2);
             multiply(first, n);
         });
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         each<kMma - kTail, kMma>([&](auto n) {
-            each<share(n - kMma + kTail, kLoadSlots, kLoads), share(n - kMma + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, dp, dq, l); });
+            each<share(n - kMma + kTail, kLoadSlots, kLoads), share(n - kMma + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, l); });
             multiply(first, n);
         });
         each<0, kMma>([&](auto n) {
             each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(other, first, f); });
-            each<share(n + kTail, kLoadSlots, kLoads), share(n + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, dp, dq, l); });
+            each<share(n + kTail, kLoadSlots, kLoads), share(n + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, l); });
             multiply(second, n);
         });
     };
     // loads past the end of r give zeros, so two steps at a time are right for any number
-    const int steps = (int)((r1 - r0 + kStep - 1) / kStep);
+    const int steps = (int)((r1 - r0 + kStep - 1) / kStep), whole = (int)((r1 - r0) / kStep);
     if (steps > 0) {
         each<0, 2>([&](auto buffer) {
-            dp = sp.open(), dq = sq.open();
+            sp.open(buffer), sq.open(buffer);
             asm volatile("s_nop 4" ::: "memory");  // a descriptor just written may not be read at once
-            each<0, kLoads>([&](auto l) { load(buffer, dp, dq, l); });
-            sp.next(), sq.next();
+            each<0, kLoads>([&](auto l) { load(buffer, l); });
         });
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
         each<0, kFrags>([&](auto f) { read(first, first, f); });
-        for (int t = 0; t < steps; t += 2) {
-            step(first);
-            step(second);
+        int t = 0;
+        for (; t + 5 < whole; t += 2) {
+            step(first, std::true_type{}, t);
+            step(second, std::true_type{}, t + 1);
+        }
+        for (; t < steps; t += 2) {
+            step(first, std::false_type{}, t);
+            step(second, std::false_type{}, t + 1);
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the last loads, before this LDS has another use
     }
