@@ -285,8 +285,8 @@ __global__ __launch_bounds__(256) void product_any(Product a, Epilogue e, int64_
 // ---------------------------------------------------------------------------
 // Tiles go from memory to LDS without passing through registers; bytes past an
 // operand's end arrive as zeros, which is how rows, columns and sums that end
-// inside a tile are handled.  Two tiles a step are in LDS: while one is read the
-// next is on its way.  A step's r is multiplied in two halves, and the fragments
+// inside a tile are handled.  LDS holds two tiles of P and three of Q: while one is
+// read the next are on their way.  A step's r is multiplied in two halves, and the fragments
 // of a half are read while the half before is multiplied, across steps too, so
 // the matrix instructions wait at one barrier a step, which stands between the
 // halves: there every wave has read all of the step's tile, whose place the
@@ -325,40 +325,46 @@ struct Wide<e4m3> {
 template <typename T, bool kDown, int kWidth>
 struct Reader {
     using frag = typename Wide<T>::frag;
-    int lane_at[2][4];  // by buffer: constants reach 2^16 bytes
-    // The wave's rows (columns) begin at w0; the operand's tile `begin` bytes into a
-    // buffer, and a buffer `size` bytes after the one before.
-    __device__ void init(int w0, int begin, int size) {
+    int lane_at[4];  // in the operand's first tile
+    int from[2][4];  // in the tile of this step and of the next (constants reach 2^16 bytes only)
+    // The wave's rows (columns) begin at w0, the operand's first tile `begin` bytes into LDS.
+    __device__ void init(int w0, int begin) {
         const int lane = threadIdx.x % 64;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             if constexpr (kDown) {  // by the 32 columns; rows of r are constants
                 const int r = (lane / 32) * 8 + (lane % 16) / 4;
-                lane_at[0][c] = begin + r * kWidth * 2 + (((w0 / 16 + 2 * c + (lane / 16) % 2) ^ down_bits(r)) << 5) + (lane % 4) * 8;
+                lane_at[c] = begin + r * kWidth * 2 + (((w0 / 16 + 2 * c + (lane / 16) % 2) ^ down_bits(r)) << 5) + (lane % 4) * 8;
             } else {  // by the pair of units
-                lane_at[0][c] = begin + along_at(w0 + lane % 32, 2 * c + lane / 32);
+                lane_at[c] = begin + along_at(w0 + lane % 32, 2 * c + lane / 32);
             }
-            lane_at[1][c] = lane_at[0][c] + size;
-            asm volatile("" : "+v"(lane_at[1][c]));  // a register of its own, not an addition at every read
+        }
+    }
+    // From now on `set` reads the tile `offset` bytes after the first.
+    __device__ void aim(int set, int offset) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            from[set][c] = lane_at[c] + offset;
+            asm volatile("" : "+v"(from[set][c]));  // a register of its own, not an addition at every read
         }
     }
     // Rows (columns) 32 n .. 32 n + 31 of the wave, instruction d of half `half`.
-    template <int buffer, int half, int d, int n>
+    template <int set, int half, int d, int n>
     __device__ frag read(const char *lds) const {
         if constexpr (sizeof(T) == 1) {
-            const i32x4 lo = *(const i32x4 *)(lds + lane_at[buffer][half * 2] + n * 32 * kStepBytes);
-            const i32x4 hi = *(const i32x4 *)(lds + lane_at[buffer][half * 2 + 1] + n * 32 * kStepBytes);
+            const i32x4 lo = *(const i32x4 *)(lds + from[set][half * 2] + n * 32 * kStepBytes);
+            const i32x4 hi = *(const i32x4 *)(lds + from[set][half * 2 + 1] + n * 32 * kStepBytes);
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         } else if constexpr (!kDown) {
-            return *(const frag *)(lds + lane_at[buffer][half * 2 + d] + n * 32 * kStepBytes);
+            return *(const frag *)(lds + from[set][half * 2 + d] + n * 32 * kStepBytes);
         } else {
             using s16x4 = vec<short, 4>;
             using s16x8 = vec<short, 8>;
             s16x4 part[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // rows of r 4 on: bit 2, which the permutation does not see
-                const char *const from = lds + lane_at[buffer][n] + (half * 32 + d * 16 + 4 * h) * kWidth * 2;
-                part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
+                const char *const at = lds + from[set][n] + (half * 32 + d * 16 + 4 * h) * kWidth * 2;
+                part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
             }
             return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
@@ -476,8 +482,8 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     constexpr int kBI = 64 * kTI, kBJ = 64 * kTJ;
     constexpr int kDeep = Wide<T>::kDeep;
     constexpr int64_t kStep = kStepBytes / sizeof(T);
-    constexpr int kTileP = kBI * kStepBytes, kTile = kTileP + kBJ * kStepBytes;
-    __shared__ __attribute__((aligned(1024))) char tiles[2][kTile];
+    constexpr int kTileP = kBI * kStepBytes, kTileQ = kBJ * kStepBytes;
+    __shared__ __attribute__((aligned(1024))) char tiles[2 * kTileP + 3 * kTileQ];
     using frag = typename Wide<T>::frag;
     int bi, bj;
     tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
@@ -493,26 +499,20 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     const int64_t r0 = (int64_t)blockIdx.y * share_steps * kStep, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kStep);
     sp.init(a.p, a.ldp, i0, a.ni, r0, r1, r1 < a.nr ? r1 * (int64_t)sizeof(T) : p_bytes);
     sq.init(a.q, a.ldq, j0, a.nj, r0, r1, r1 * (int64_t)sizeof(T));
-    rp.init(wi, 0, kTile);
-    rq.init(wj, kTileP, kTile);
-    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&tiles[0][0];
-    const unsigned to_p = lds + wave * sp.kLoads * 1024, to_q = lds + kTileP + wave * sq.kLoads * 1024;
+    rp.init(wi, 0);
+    rq.init(wj, 2 * kTileP);
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&tiles[0];
+    const unsigned to_p = lds + wave * sp.kLoads * 1024, to_q = lds + 2 * kTileP + wave * sq.kLoads * 1024;
     f32x16 acc[kTI][kTJ] = {};
     frag p[2][kDeep][kTI], q[2][kDeep][kTJ];
-    // Load l, fragment f and matrix instruction n, each in the order of use.
-    constexpr int kLoads = sp.kLoads + sq.kLoads, kFrags = kDeep * (kTI + kTJ), kMma = kDeep * kTI * kTJ;
-    const auto load = [&](auto buffer, auto l) {
-        if constexpr (l < sp.kLoads)
-            sp.template load<l>(to_p + buffer * kTile);
-        else
-            sq.template load<l - sp.kLoads>(to_q + buffer * kTile);
-    };
-    const auto read = [&](auto buffer, auto half, auto f) {
+    // Fragment f and matrix instruction n of a half, in the order of use.
+    constexpr int kFrags = kDeep * (kTI + kTJ), kMma = kDeep * kTI * kTJ;
+    const auto read = [&](auto set, auto half, auto f) {
         constexpr int d = f / (kTI + kTJ), n = f % (kTI + kTJ);
         if constexpr (n < kTJ)
-            q[half][d][n] = rq.template read<buffer, half, d, n>(&tiles[0][0]);
+            q[half][d][n] = rq.template read<set, half, d, n>(&tiles[0]);
         else
-            p[half][d][n - kTJ] = rp.template read<buffer, half, d, n - kTJ>(&tiles[0][0]);
+            p[half][d][n - kTJ] = rp.template read<set, half, d, n - kTJ>(&tiles[0]);
     };
     const auto multiply = [&](auto half, auto n) {
         constexpr int d = n / (kTI * kTJ), x = n / kTJ % kTI, y = n % kTJ;
@@ -522,49 +522,69 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
     // The barrier comes before the last kTail instructions of the first half, so
-    // that they keep the matrix unit busy while the waves meet; a slot is the gap
-    // before a matrix instruction, and little may stand in it: there is one wave to
-    // a SIMD, an instruction takes it some 4 cycles, a matrix instruction 32.
-    constexpr int kTail = kMma / 8, kReadSlots = kMma * 5 / 8, kLoadSlots = kMma * 3 / 4;
+    // that they keep the matrix unit busy while the waves meet.  From there to the
+    // next one P's tile of step t + 2 is loaded first and Q's of step t + 3 after it,
+    // which the next barrier does not wait for.  A slot is the gap before a matrix
+    // instruction, and little may stand in it: there is one wave to a SIMD, any
+    // instruction takes it some 4 cycles, a matrix instruction 32.
+    constexpr int kTail = kMma / 8, kReadSlots = kMma * 5 / 8, kSlotsP = (kMma + kTail) / 2, kSlotsQ = kMma + kTail - kSlotsP;
     static_assert(kReadSlots + 2 <= kMma - kTail, "the descriptors are made between the reads and the barrier");
-    // Step t, from buffer `now`; `inner`: step t + 2 is one that advance() may reach.
-    const auto step = [&](auto now, auto inner, int t) {
-        constexpr std::integral_constant<int, 1 - now> other{};
+    // Step t, whose tiles of P and Q are in places `now` and `place`; `inner`: steps
+    // t + 2 and t + 3 are ones that advance() may reach.
+    const auto step = [&](auto now, auto inner, int t, int place) {
+        const int after = place == 2 ? 0 : place + 1;
         each<0, kMma - kTail>([&](auto n) {
             each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(now, second, f); });
+            if constexpr (n == 0) rq.aim(1 - now, after * kTileQ);
             if constexpr (n == kReadSlots) inner ? sp.advance() : sp.open(t + 2);
-            if constexpr (n == kReadSlots + 1) inner ? sq.advance() : sq.open(t + 2);
+            if constexpr (n == kReadSlots + 1) inner ? sq.advance() : sq.open(t + 3);
             multiply(first, n);
         });
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(sq.kLoads) : "memory");
+        const auto load = [&](auto slot) {
+            each<share(slot, kSlotsP, sp.kLoads), share(slot + 1, kSlotsP, sp.kLoads)>([&](auto l) { sp.template load<l>(to_p + now * kTileP); });
+            if constexpr (slot >= kSlotsP)
+                each<share(slot - kSlotsP, kSlotsQ, sq.kLoads), share(slot - kSlotsP + 1, kSlotsQ, sq.kLoads)>(
+                    [&](auto l) { sq.template load<l>(to_q + place * kTileQ); });
+        };
         each<kMma - kTail, kMma>([&](auto n) {
-            each<share(n - kMma + kTail, kLoadSlots, kLoads), share(n - kMma + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, l); });
+            load(std::integral_constant<int, n - kMma + kTail>{});
             multiply(first, n);
         });
         each<0, kMma>([&](auto n) {
-            each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(other, first, f); });
-            each<share(n + kTail, kLoadSlots, kLoads), share(n + kTail + 1, kLoadSlots, kLoads)>([&](auto l) { load(now, l); });
+            each<share(n, kReadSlots, kFrags), share(n + 1, kReadSlots, kFrags)>([&](auto f) { read(std::integral_constant<int, 1 - now>{}, first, f); });
+            load(std::integral_constant<int, n + kTail>{});
             multiply(second, n);
         });
+        return after;
     };
     // loads past the end of r give zeros, so two steps at a time are right for any number
     const int steps = (int)((r1 - r0 + kStep - 1) / kStep), whole = (int)((r1 - r0) / kStep);
     if (steps > 0) {
-        each<0, 2>([&](auto buffer) {
-            sp.open(buffer), sq.open(buffer);
+        const auto load_p = [&](auto h) {
+            sp.open(h);
             asm volatile("s_nop 4" ::: "memory");  // a descriptor just written may not be read at once
-            each<0, kLoads>([&](auto l) { load(buffer, l); });
-        });
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            each<0, sp.kLoads>([&](auto l) { sp.template load<l>(to_p + h * kTileP); });
+        };
+        const auto load_q = [&](auto h) {
+            sq.open(h);
+            asm volatile("s_nop 4" ::: "memory");
+            each<0, sq.kLoads>([&](auto l) { sq.template load<l>(to_q + h * kTileQ); });
+        };
+        load_p(first), load_q(first);
+        load_p(second), load_q(second);
+        load_q(std::integral_constant<int, 2>{});
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(sp.kLoads + 2 * sq.kLoads) : "memory");
+        rp.aim(0, 0), rp.aim(1, kTileP), rq.aim(0, 0);
         each<0, kFrags>([&](auto f) { read(first, first, f); });
-        int t = 0;
-        for (; t + 5 < whole; t += 2) {
-            step(first, std::true_type{}, t);
-            step(second, std::true_type{}, t + 1);
+        int t = 0, place = 0;
+        for (; t + 6 < whole; t += 2) {
+            place = step(first, std::true_type{}, t, place);
+            place = step(second, std::true_type{}, t + 1, place);
         }
         for (; t < steps; t += 2) {
-            step(first, std::false_type{}, t);
-            step(second, std::false_type{}, t + 1);
+            place = step(first, std::false_type{}, t, place);
+            place = step(second, std::false_type{}, t + 1, place);
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the last loads, before this LDS has another use
     }
@@ -574,7 +594,7 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     // different banks, and come back 8 columns a lane, whole rows side by side.
     __syncthreads();
     constexpr int kRow = 32 * kTJ + 4;
-    float *const rows = (float *)&tiles[0][0] + wave * 32 * kRow;
+    float *const rows = (float *)&tiles[0] + wave * 32 * kRow;
 #pragma unroll
     for (int x = 0; x < kTI; ++x) {
 #pragma unroll
