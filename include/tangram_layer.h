@@ -59,7 +59,8 @@ typedef enum { TG_ACT_NONE = 0, TG_ACT_RELU = 1, TG_ACT_SILU = 2, TG_ACT_GELU = 
  *             is added (both or neither); NULL otherwise
  *   bias      [n] or NULL; residual [m, n] or NULL
  *   pre       [m, n] or NULL: receives z, which tg_linear_grad takes
- * residual may be y itself (added in place).  m, n, k < 2^31.
+ * residual may be y itself (added in place).  m < 2^31 - 256, n and k at most
+ * 2^21 - 64.
  */
 typedef struct {
     const void *x, *w;
@@ -71,8 +72,10 @@ typedef struct {
     int32_t type, out_type, act, reserved; /* reserved must be 0 */
 } tg_linear_args;
 
-/* Bytes of workspace that tg_linear wants for these sizes and types (0 where
-   it needs none, or where the arguments are invalid).  Pointers are not read. */
+/* Bytes of workspace that tg_linear wants for these arguments (0 where it needs
+   none, or where they are invalid): operands that do not start at 16-byte
+   addresses are copied there first, and sums that are shared out among blocks
+   meet there.  Nothing is read through the pointers. */
 size_t tg_linear_workspace_bytes(const tg_linear_args *a);
 tg_status tg_linear(const tg_linear_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
 

@@ -32,50 +32,19 @@ __device__ inline int down_bits(int r) { return (r & 3) | ((r >> 1) & 4); }
 // The wave's number, known to the compiler to be the same in all its lanes.
 __device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
 
+// 16 x 16 matrix instructions: a lane holds 8 elements of row lane % 16.
 template <typename T>
 struct Matrix;
 template <>
 struct Matrix<bf16> {
-    static constexpr int kSub = 2;  // matrix instructions along a step's r
     using frag = vec<bf16, 8>;
     static __device__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <>
 struct Matrix<f16> {
-    static constexpr int kSub = 2;
     using frag = vec<f16, 8>;
     static __device__ f32x4 mma(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
-// Lane l's part of rows row0 .. row0 + 15: 16 bytes of row l % 16.
-// Which r a lane holds does not matter as long as P and Q agree.
-template <typename T>
-__device__ inline typename Matrix<T>::frag read_along(const char *tile, int row0, int sub) {
-    const int lane = threadIdx.x % 64, row = row0 + lane % 16;
-    return *(const typename Matrix<T>::frag *)(tile + along_at(row, sub * 4 + lane / 16));
-}
-// The same from a "down" tile of `width` columns: the transposing load hands each
-// lane of 16 one column of the 4 x 16 block whose rows the lanes point at.
-template <typename T>
-__device__ inline typename Matrix<T>::frag read_down(const char *tile, int col0, int sub, int width) {
-    using s16x4 = vec<short, 4>;
-    const int lane = threadIdx.x % 64, r = sub * 32 + (lane / 16) * 8 + (lane % 16) / 4;
-    s16x4 half[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int at = (r + 4 * h) * width * 2 + (((col0 / 16) ^ down_bits(r + 4 * h)) << 5) + (lane % 4) * 8;
-        half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(tile + at));
-    }
-    using s16x8 = vec<short, 8>;
-    return __builtin_bit_cast(typename Matrix<T>::frag, (s16x8)__builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7));
-}
-template <typename T, bool kDown>
-__device__ inline typename Matrix<T>::frag read_frag(const char *tile, int at, int sub, int width) {
-    if constexpr (kDown)
-        return read_down<T>(tile, at, sub, width);
-    else
-        return read_along<T>(tile, at, sub);
-}
-
 // ---------------------------------------------------------------------------
 // epilogue
 // ---------------------------------------------------------------------------
@@ -148,7 +117,7 @@ __device__ inline void finish(vec<float, N> z, int64_t i, int64_t j, int valid, 
 }
 
 // ---------------------------------------------------------------------------
-// the product for operands at any alignment
+// operands
 // ---------------------------------------------------------------------------
 struct Product {
     const void *p, *q;
@@ -185,99 +154,6 @@ __device__ inline i32x4 widened(vec<int, 2> u) {
         r[2 * h + 1] = __builtin_bit_cast(int, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[h], 1.0f, true));
     }
     return r;
-}
-
-constexpr int kAnyTile = 128;
-constexpr int kAnyUnits = kAnyTile * kStepBytes / 16 / 256;  // units of a tile each thread moves
-
-template <typename T, bool kDown>
-__device__ inline void fetch(typename Unit<T>::raw (&u)[kAnyUnits], const T *base, int64_t ld, int64_t at0, int64_t n_at, int64_t r0,
-                             int64_t nr) {
-#pragma unroll
-    for (int n = 0; n < kAnyUnits; ++n) {
-        const int c = threadIdx.x + n * 256;
-        if constexpr (kDown) {  // 16 units a row of r
-            const int64_t r = r0 + c / 16, at = at0 + (c % 16) * 8;
-            u[n] = Unit<T>::load(base + r * ld + at, r < nr ? n_at - at : 0);
-        } else {  // 8 units a row
-            const int64_t at = at0 + c / 8, r = r0 + (c % 8) * 8;
-            u[n] = Unit<T>::load(base + at * ld + r, at < n_at ? nr - r : 0);
-        }
-    }
-}
-template <typename T, bool kDown>
-__device__ inline void place(const typename Unit<T>::raw (&u)[kAnyUnits], char *tile) {
-#pragma unroll
-    for (int n = 0; n < kAnyUnits; ++n) {
-        const int c = threadIdx.x + n * 256;
-        if constexpr (kDown) {
-            const int r = c / 16, unit = c % 16;
-            *(i32x4 *)(tile + r * kAnyTile * 2 + ((((unit >> 1) ^ down_bits(r)) << 5) | ((unit & 1) << 4))) = widened(u[n]);
-        } else {
-            *(i32x4 *)(tile + along_at(c / 8, c % 8)) = widened(u[n]);
-        }
-    }
-}
-
-// 128 x 128 of C by four waves of 64 x 64.  Units pass through registers, so
-// rows may start anywhere and end inside a unit; the next step's are on their
-// way while this step's are multiplied.  8-bit operands become bf16 on the way,
-// which is exact: the 8-bit matrix instruction's own sums are not (see there).
-template <typename T, typename O, bool kDownP, bool kDownQ>
-__global__ __launch_bounds__(256) void product_any(Product a, Epilogue e, int64_t tiles_j) {
-    __shared__ __attribute__((aligned(16))) char tile_p[2][kAnyTile * kStepBytes], tile_q[2][kAnyTile * kStepBytes];
-    using C = std::conditional_t<sizeof(T) == 1, bf16, T>;
-    constexpr int kStep = kStepBytes / 2;
-    const int64_t i0 = blockIdx.x / tiles_j * kAnyTile, j0 = blockIdx.x % tiles_j * kAnyTile;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    const int wi = (wave / 2) * 64, wj = (wave % 2) * 64;
-    f32x4 acc[4][4] = {};
-    typename Unit<T>::raw up[kAnyUnits], uq[kAnyUnits];
-    const int64_t steps = (a.nr + kStep - 1) / kStep;
-    if (steps > 0) {
-        fetch<T, kDownP>(up, (const T *)a.p, a.ldp, i0, a.ni, 0, a.nr);
-        fetch<T, kDownQ>(uq, (const T *)a.q, a.ldq, j0, a.nj, 0, a.nr);
-        place<T, kDownP>(up, tile_p[0]);
-        place<T, kDownQ>(uq, tile_q[0]);
-        __syncthreads();
-    }
-    for (int64_t t = 0; t < steps; ++t) {
-        const bool more = t + 1 < steps;
-        if (more) {
-            fetch<T, kDownP>(up, (const T *)a.p, a.ldp, i0, a.ni, (t + 1) * kStep, a.nr);
-            fetch<T, kDownQ>(uq, (const T *)a.q, a.ldq, j0, a.nj, (t + 1) * kStep, a.nr);
-        }
-        const char *const tp = tile_p[t & 1], *const tq = tile_q[t & 1];
-#pragma unroll
-        for (int sub = 0; sub < Matrix<C>::kSub; ++sub) {
-            typename Matrix<C>::frag p[4], q[4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                p[n] = read_frag<C, kDownP>(tp, wi + n * 16, sub, kAnyTile);
-                q[n] = read_frag<C, kDownQ>(tq, wj + n * 16, sub, kAnyTile);
-            }
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) acc[x][y] = Matrix<C>::mma(q[y], p[x], acc[x][y]);
-        }
-        if (more) {
-            place<T, kDownP>(up, tile_p[(t + 1) & 1]);
-            place<T, kDownQ>(uq, tile_q[(t + 1) & 1]);
-        }
-        __syncthreads();
-    }
-    // a lane has columns 4 (lane / 16) .. + 3 of row lane % 16 of each 16 x 16 part
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const int64_t i = i0 + wi + x * 16 + lane % 16;
-        if (i >= a.ni) continue;
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const int64_t j = j0 + wj + y * 16 + (lane / 16) * 4;
-            if (j < a.nj) finish<O, 4>(acc[x][y], i, j, (int)std::min<int64_t>(4, a.nj - j), e);
-        }
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -477,8 +353,8 @@ constexpr int share(int n, int slots, int of) { return n >= slots ? of : (n * of
 
 // 64 kTI x 64 kTJ of C by four waves of 32 kTI x 32 kTJ.
 template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ>
-__global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t p_bytes,
-                                                                             int share_steps) {
+__global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p,
+                                                                             int64_t r_bytes_q, int share_steps) {
     constexpr int kBI = 64 * kTI, kBJ = 64 * kTJ;
     constexpr int kDeep = Wide<T>::kDeep;
     constexpr int64_t kStep = kStepBytes / sizeof(T);
@@ -497,8 +373,8 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     Reader<T, kDownQ, kBJ> rq;
     // this block's share of r: all of it where there are no splits
     const int64_t r0 = (int64_t)blockIdx.y * share_steps * kStep, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kStep);
-    sp.init(a.p, a.ldp, i0, a.ni, r0, r1, r1 < a.nr ? r1 * (int64_t)sizeof(T) : p_bytes);
-    sq.init(a.q, a.ldq, j0, a.nj, r0, r1, r1 * (int64_t)sizeof(T));
+    sp.init(a.p, a.ldp, i0, a.ni, r0, r1, r1 < a.nr ? r1 * (int64_t)sizeof(T) : r_bytes_p);
+    sq.init(a.q, a.ldq, j0, a.nj, r0, r1, r1 < a.nr ? r1 * (int64_t)sizeof(T) : r_bytes_q);
     rp.init(wi, 0);
     rq.init(wj, 2 * kTileP);
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&tiles[0];
@@ -704,6 +580,8 @@ __global__ __launch_bounds__(256) void join_kernel(Epilogue e, int splits, int64
     finish<O, 8>(z, i, j, valid, e);
 }
 
+constexpr int64_t kMostLd = 1 << 21;  // elements of a row of a product's operands
+
 // How a product is cut: tiles of 256 or 128, and r into splits, whichever is
 // estimated to take the least time.  Measured, in us: a step of a 256 tile takes
 // 1.35 while few of the 256 CUs work and 1.8 when all do (8192^3: 1.75), one of a
@@ -720,7 +598,7 @@ Cut cut_product(int64_t ni, int64_t nj, int64_t nr, int size) {
     Cut best{256, 1, (int)steps};
     double least = 0;
     for (int tile = 256; tile >= 128; tile /= 2) {
-        for (int want = 1; want <= 8 && (want == 1 || steps / want >= 4); ++want) {
+        for (int want = 1; want <= 8 && (want == 1 || (steps / want >= 4 && ni * nj <= 1 << 26)); ++want) {
             const int share = want == 1 ? (int)steps : (int)(ceil_div(ceil_div(steps, want), 2) * 2);
             const int splits = (int)ceil_div(steps, share);
             const int64_t blocks = ceil_div(ni, tile) * ceil_div(nj, tile) * splits;
@@ -737,25 +615,75 @@ Cut cut_product(int64_t ni, int64_t nj, int64_t nr, int size) {
 }
 size_t cut_bytes(const Cut &c, int64_t ni, int64_t nj) { return c.splits > 1 ? round256((size_t)c.splits * ni * nj * 4) : 0; }
 
+// Rows into rows that start at 16-byte addresses and end in zeros on a whole unit
+// of 16 bytes, for one operand or two.  Bound by memory, 4 TB/s read and written
+// together; reading unaligned rows in the product itself took 2.5 to 4.7 us a
+// step of 128 tiles where aligned ones take 0.65 to 1.05.
+struct Packing {
+    const void *from[2];
+    void *to[2];
+    int64_t rows[2], cols[2], ld[2], ld_to[2];  // rows 0: none
+};
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(Packing a) {
+    constexpr int kN = 16 / sizeof(T);
+    const int o = blockIdx.y;
+    const int64_t units = a.ld_to[o] / kN, all = a.rows[o] * units;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < all; u += (int64_t)gridDim.x * 256) {
+        const int64_t row = u / units, col = u % units * kN;
+        const T *const from = (const T *)a.from[o] + row * a.ld[o] + col;
+        vec<T, kN> v;
+        if (a.cols[o] - col >= kN) {
+            v = load_loose<T, kN>(from);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) v[e] = col + e < a.cols[o] ? from[e] : (T)0;
+        }
+        *(vec<T, kN> *)((T *)a.to[o] + row * a.ld_to[o] + col) = v;
+    }
+}
+
 // Whether operand rows start at 16-byte addresses, an operand with r along its
 // rows ends on a whole unit (`r_bytes` of each row may be read), and a tile's
 // offsets fit 31 bits.
-template <typename T>
-bool streams(const void *p, int64_t ld, int64_t rows, int64_t r_bytes, bool down) {
-    const int64_t row_bytes = ld * (int64_t)sizeof(T);
-    return (uintptr_t)p % 16 == 0 && (rows < 2 || row_bytes % 16 == 0) && (down || r_bytes % 16 == 0) && row_bytes < (1 << 22);
+bool streams(const void *p, int64_t ld, int size, int64_t r_bytes, bool down) {
+    return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0 && (down || r_bytes % 16 == 0) && ld < kMostLd;
+}
+int64_t whole_ld(int64_t cols, int size) { return ceil_div(cols * size, 16) * 16 / size; }
+
+// How a product is done: the kernel, the operands that are packed first, and what
+// lies where in the workspace: packed P, packed Q, shares.
+struct Plan {
+    bool few, pack_p, pack_q;
+    Cut cut;
+    size_t p_bytes, q_bytes, bytes;
+};
+Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bool down_q) {
+    Plan p{};
+    if (a.ni == 0 || a.nj == 0) return p;
+    p.pack_p = !streams(a.p, a.ldp, size, r_bytes_p, down_p);
+    p.pack_q = !streams(a.q, a.ldq, size, a.nr * size, down_q);
+    // From some 8 rows on tiles of 128 and splits are as fast: 4096 x 14336 in
+    // bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at 16.
+    // Where an operand would have to be packed, up to 64 rows.
+    p.few = !down_p && !down_q && a.ni <= (p.pack_p || p.pack_q ? 64 : 8);
+    if (p.few) return p;
+    p.cut = cut_product(a.ni, a.nj, a.nr, size);
+    const auto packed = [&](int64_t n, bool down) { return round256(down ? a.nr * whole_ld(n, size) * size : n * whole_ld(a.nr, size) * size); };
+    p.p_bytes = p.pack_p ? packed(a.ni, down_p) : 0;
+    p.q_bytes = p.pack_q ? packed(a.nj, down_q) : 0;
+    p.bytes = p.p_bytes + p.q_bytes + cut_bytes(p.cut, a.ni, a.nj);
+    return p;
 }
 
-// C by the kernel that its operands' alignment allows; `ws` holds cut_bytes.
+// C; `ws` holds the plan's bytes.
 template <typename T, typename O, bool kDownP, bool kDownQ>
-hipError_t launch_product(const Product &a, Epilogue e, int64_t p_bytes, void *ws, hipStream_t s) {
+hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hipStream_t s) {
+    constexpr int kSize = sizeof(T);
     if (a.ni == 0 || a.nj == 0) return hipSuccess;
-    const bool direct = streams<T>(a.p, a.ldp, kDownP ? a.nr : a.ni, p_bytes, kDownP) &&
-                        streams<T>(a.q, a.ldq, kDownQ ? a.nr : a.nj, a.nr * (int64_t)sizeof(T), kDownQ);
+    const Plan p = plan_product(a, kSize, r_bytes_p, kDownP, kDownQ);
     if constexpr (!kDownP && !kDownQ) {
-        // From some 8 rows on tiles of 128 and splits are as fast: 4096 x 14336 in
-        // bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at 16.
-        if (a.ni <= (direct ? 8 : 64)) {
+        if (p.few) {
             const dim3 grid((unsigned)ceil_div(a.nj, 16));
             switch ((a.ni + 15) / 16) {
                 case 1: hipLaunchKernelGGL((product_few<T, O, 1>), grid, dim3(512), 0, s, a, e); break;
@@ -766,24 +694,36 @@ hipError_t launch_product(const Product &a, Epilogue e, int64_t p_bytes, void *w
             return hipGetLastError();
         }
     }
-    if (direct) {
-        const Cut c = cut_product(a.ni, a.nj, a.nr, sizeof(T));
-        e.partial = c.splits > 1 ? (float *)ws : nullptr;
-        const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, c.tile);
-        const dim3 grid(ti * tj, c.splits);
-        if (c.tile == 256)
-            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4>), grid, dim3(256), 0, s, a, e, ti, tj, p_bytes, c.share);
-        else
-            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2>), grid, dim3(256), 0, s, a, e, ti, tj, p_bytes, c.share);
-        if (e.partial) {
-            const hipError_t r = hipGetLastError();
-            if (r != hipSuccess) return r;
-            hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)ceil_div(a.ni * ceil_div(a.nj, 8), 256)), dim3(256), 0, s, e, c.splits, a.ni, a.nj);
-        }
-        return hipGetLastError();
+    if ((p.pack_p || p.pack_q) && a.nr > 0) {
+        Packing k{};
+        const auto pack = [&](int o, const void *&from, int64_t &ld, int64_t n, bool down, char *to) {
+            k.from[o] = from, k.to[o] = to, k.ld[o] = ld;
+            k.rows[o] = down ? a.nr : n, k.cols[o] = down ? n : a.nr;
+            k.ld_to[o] = ld = whole_ld(k.cols[o], kSize);
+            from = to;
+        };
+        if (p.pack_p) pack(0, a.p, a.ldp, a.ni, kDownP, ws), r_bytes_p = a.ldp * kSize;
+        if (p.pack_q) pack(1, a.q, a.ldq, a.nj, kDownQ, ws + p.p_bytes);
+        const int64_t units = std::max(k.rows[0] * k.ld_to[0], k.rows[1] * k.ld_to[1]) * kSize / 16;
+        using Moved = std::conditional_t<kSize == 1, unsigned char, T>;
+        hipLaunchKernelGGL(pack_kernel<Moved>, dim3((unsigned)std::min<int64_t>(2048, ceil_div(units, 256)), 2), dim3(256), 0, s, k);
+        const hipError_t r = hipGetLastError();
+        if (r != hipSuccess) return r;
     }
-    const int64_t ti = ceil_div(a.ni, kAnyTile), tj = ceil_div(a.nj, kAnyTile);
-    hipLaunchKernelGGL((product_any<T, O, kDownP, kDownQ>), dim3((unsigned)(ti * tj)), dim3(256), 0, s, a, e, tj);
+    const int64_t r_bytes_q = p.pack_q ? a.ldq * kSize : a.nr * kSize;
+    const Cut &c = p.cut;
+    e.partial = c.splits > 1 ? (float *)(ws + p.p_bytes + p.q_bytes) : nullptr;
+    const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, c.tile);
+    const dim3 grid(ti * tj, c.splits);
+    if (c.tile == 256)
+        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
+    else
+        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
+    if (e.partial) {
+        const hipError_t r = hipGetLastError();
+        if (r != hipSuccess) return r;
+        hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)ceil_div(a.ni * ceil_div(a.nj, 8), 256)), dim3(256), 0, s, e, c.splits, a.ni, a.nj);
+    }
     return hipGetLastError();
 }
 
@@ -861,70 +801,81 @@ tg_status check_workspace(const void *ws, size_t bytes, size_t need) {
 }
 
 bool sizes_fit(int64_t m, int64_t n, int64_t k) {
-    const int64_t most = 0x7fffffff - 256;
-    return m >= 0 && n >= 0 && k >= 0 && m <= most && n <= most && k <= most &&
-           ceil_div(m, kAnyTile) * ceil_div(std::max(n, k), kAnyTile) < (1 << 24) &&
-           ceil_div(n, kAnyTile) * ceil_div(k, kAnyTile) < (1 << 24);
+    const int64_t most = kMostLd - 64;
+    return m >= 0 && n >= 0 && k >= 0 && m <= 0x7fffffff - 256 && n <= most && k <= most &&
+           // a grid holds fewer than 2^32 threads
+           ceil_div(m, 128) * ceil_div(std::max(n, k), 128) < (1 << 24) && ceil_div(n, 128) * ceil_div(k, 128) < (1 << 24) &&
+           m * ceil_div(std::max(n, k), 8) < (int64_t)1 << 32;
 }
+
+// A row stride that may be used where there are fewer than two rows, too.
+int64_t ld_of(int64_t ld, int64_t rows, int64_t cols, int type) { return rows < 2 ? whole_ld(cols, (int)size_of(type)) : ld; }
 
 bool valid_types(int type, int out_type) {
     if (type == TG_E4M3) return out_type == TG_BF16 || out_type == TG_F16;
     return (type == TG_BF16 || type == TG_F16) && out_type == type;
 }
 
+// What tg_linear_grad does, and what lies where in its workspace: dz, sums, and
+// the place of the two products, which run one after the other.
 struct GradPlan {
-    bool slope, sums;  // dz differs from dy; a bias's gradient is wanted
+    bool slope, sums;  // dz is not dy where it lies; a bias's gradient is wanted
     int64_t ldz;
     int rows;
-    size_t dz_bytes, sum_bytes, cut_bytes;
-    size_t bytes() const { return dz_bytes + sum_bytes + cut_bytes; }
+    size_t dz_bytes, sum_bytes, product_bytes;
+    Product dx, dw;
+    size_t bytes() const { return dz_bytes + sum_bytes + product_bytes; }
 };
 
-GradPlan plan_grad(const tg_linear_grad_args &q) {
-    GradPlan p;
-    p.slope = q.act != TG_ACT_NONE && (q.dx || q.dw);
+GradPlan plan_grad(const tg_linear_grad_args &q, char *ws) {
+    GradPlan p{};
+    const int64_t lddy = ld_of(q.lddy, q.m, q.n, q.type);
+    // dy is read as it lies where there is no activation and its rows are aligned
+    p.slope = (q.dx || q.dw) && (q.act != TG_ACT_NONE || !streams(q.dy, lddy, 2, q.n * 2, false));
     p.sums = q.dbias != nullptr;
-    p.ldz = ceil_div(q.n, 8) * 8;
+    p.ldz = p.slope ? whole_ld(q.n, 2) : lddy;
     p.rows = slope_rows(q.m, q.n);
     p.dz_bytes = p.slope ? round256((size_t)q.m * p.ldz * 2) : 0;
     p.sum_bytes = p.sums ? round256((size_t)p.rows * q.n * 4) : 0;
-    // the two products run one after the other in the same place
-    p.cut_bytes = 0;
-    if (q.dx) p.cut_bytes = cut_bytes(cut_product(q.m, q.k, q.n, 2), q.m, q.k);
-    if (q.dw) p.cut_bytes = std::max(p.cut_bytes, cut_bytes(cut_product(q.n, q.k, q.m, 2), q.n, q.k));
+    const void *const dz = p.slope ? ws : q.dy;
+    p.dx = Product{dz, q.w, p.ldz, ld_of(q.ldw, q.n, q.k, q.type), q.m, q.k, q.n};
+    p.dw = Product{dz, q.x, p.ldz, ld_of(q.ldx, q.m, q.k, q.type), q.n, q.k, q.m};
+    if (q.dx) p.product_bytes = plan_product(p.dx, 2, (p.slope ? p.ldz * 2 : q.n * 2), false, true).bytes;
+    if (q.dw) p.product_bytes = std::max(p.product_bytes, plan_product(p.dw, 2, 0, true, true).bytes);
     return p;
 }
 
 template <typename E>
 tg_status run_grad(const tg_linear_grad_args &q, const GradPlan &p, char *ws, hipStream_t s) {
-    const void *dz = q.dy;
-    int64_t ldz = q.lddy;
-    void *const shares = ws + p.dz_bytes + p.sum_bytes;
+    char *const place = ws + p.dz_bytes + p.sum_bytes;
+    float *const sums = (float *)(ws + p.dz_bytes);
     if ((p.slope || p.sums) && q.m > 0 && q.n > 0) {
-        SlopeArgs a{q.dy, q.pre, p.slope ? ws : nullptr, p.sums ? (float *)(ws + p.dz_bytes) : nullptr,
-                    q.m, q.n, q.lddy, q.ldp, p.ldz, q.act};
+        SlopeArgs a{q.dy, q.pre, p.slope ? ws : nullptr, p.sums ? sums : nullptr, q.m, q.n, q.lddy, q.ldp, p.ldz, q.act};
         hipLaunchKernelGGL(slope_kernel<E>, dim3((unsigned)ceil_div(q.n, 256), p.rows), dim3(256), 0, s, a);
-        hipError_t e = hipGetLastError();
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return device_failed(e, "slope_kernel");
-        if (p.slope) dz = ws, ldz = p.ldz;
     }
     if (p.sums) {
-        const hipError_t e = launch_column_sums((const float *)(ws + p.dz_bytes), q.m > 0 ? p.rows : 0, q.n, q.dbias, q.type, s);
+        const hipError_t e = launch_column_sums(sums, q.m > 0 ? p.rows : 0, q.n, q.dbias, q.type, s);
         if (e != hipSuccess) return device_failed(e, "column_sums");
     }
     if (q.dx) {
         Epilogue e{};
         e.out = q.dx, e.ldo = q.lddx;
-        const hipError_t r = launch_product<E, E, false, true>(Product{dz, q.w, ldz, q.ldw, q.m, q.k, q.n}, e, p.slope ? ldz * 2 : q.n * 2, shares, s);
+        const hipError_t r = launch_product<E, E, false, true>(p.dx, e, (p.slope ? p.ldz * 2 : q.n * 2), place, s);
         if (r != hipSuccess) return device_failed(r, "the product dz w");
     }
     if (q.dw) {
         Epilogue e{};
         e.out = q.dw, e.ldo = q.lddw;
-        const hipError_t r = launch_product<E, E, true, true>(Product{dz, q.x, ldz, q.ldx, q.n, q.k, q.m}, e, 0, shares, s);
+        const hipError_t r = launch_product<E, E, true, true>(p.dw, e, 0, place, s);
         if (r != hipSuccess) return device_failed(r, "the product dz^T x");
     }
     return TG_OK;
+}
+
+Product forward_product(const tg_linear_args &q) {
+    return Product{q.x, q.w, ld_of(q.ldx, q.m, q.k, q.type), ld_of(q.ldw, q.n, q.k, q.type), q.m, q.n, q.k};
 }
 
 }  // namespace
@@ -942,7 +893,8 @@ extern "C" {
 
 size_t tg_linear_workspace_bytes(const tg_linear_args *q) {
     if (!q || !sizes_fit(q->m, q->n, q->k) || !valid_types(q->type, q->out_type)) return 0;
-    return cut_bytes(cut_product(q->m, q->n, q->k, (int)size_of(q->type)), q->m, q->n);
+    const int size = (int)size_of(q->type);
+    return plan_product(forward_product(*q), size, q->k * size, false, false).bytes;
 }
 
 tg_status tg_linear(const tg_linear_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
@@ -963,25 +915,25 @@ tg_status tg_linear(const tg_linear_args *q, void *d_ws, size_t ws_bytes, tg_str
     if (q->x_scale) TG_TRY(check_matrix(q->x_scale, 0, 1, q->m, TG_F32, "x_scale"));
     if (q->w_scale) TG_TRY(check_matrix(q->w_scale, 0, 1, q->n, TG_F32, "w_scale"));
     TG_TRY(check_workspace(d_ws, ws_bytes, tg_linear_workspace_bytes(q)));
-    const Product a{q->x, q->w, q->ldx, q->ldw, q->m, q->n, q->k};
+    const Product a = forward_product(*q);
     const Epilogue e{q->x_scale, q->w_scale, q->bias, q->residual, q->y, q->pre, q->ldr, q->ldy, q->ldp, q->act, nullptr};
     const hipStream_t s = (hipStream_t)stream;
-    const int64_t x_bytes = q->k * (q->type == TG_E4M3 ? 1 : 2);
+    char *const ws = (char *)d_ws;
     hipError_t r;
     if (q->type == TG_BF16)
-        r = launch_product<bf16, bf16, false, false>(a, e, x_bytes, d_ws, s);
+        r = launch_product<bf16, bf16, false, false>(a, e, q->k * 2, ws, s);
     else if (q->type == TG_F16)
-        r = launch_product<f16, f16, false, false>(a, e, x_bytes, d_ws, s);
+        r = launch_product<f16, f16, false, false>(a, e, q->k * 2, ws, s);
     else if (q->out_type == TG_BF16)
-        r = launch_product<e4m3, bf16, false, false>(a, e, x_bytes, d_ws, s);
+        r = launch_product<e4m3, bf16, false, false>(a, e, q->k, ws, s);
     else
-        r = launch_product<e4m3, f16, false, false>(a, e, x_bytes, d_ws, s);
+        r = launch_product<e4m3, f16, false, false>(a, e, q->k, ws, s);
     return r == hipSuccess ? TG_OK : device_failed(r, "the product x w^T");
 }
 
 size_t tg_linear_grad_workspace_bytes(const tg_linear_grad_args *q) {
     if (!q || !sizes_fit(q->m, q->n, q->k)) return 0;
-    return plan_grad(*q).bytes();
+    return plan_grad(*q, nullptr).bytes();
 }
 
 tg_status tg_linear_grad(const tg_linear_grad_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
@@ -1001,7 +953,7 @@ tg_status tg_linear_grad(const tg_linear_grad_args *q, void *d_ws, size_t ws_byt
         TG_TRY(check_matrix(q->dx, q->lddx, q->m, q->k, q->type, "dx"));
     }
     if (q->dbias) TG_TRY(check_matrix(q->dbias, 0, 1, q->n, q->type, "dbias"));
-    const GradPlan p = plan_grad(*q);
+    const GradPlan p = plan_grad(*q, (char *)d_ws);
     TG_TRY(check_workspace(d_ws, ws_bytes, p.bytes()));
     return q->type == TG_BF16 ? run_grad<bf16>(*q, p, (char *)d_ws, (hipStream_t)stream)
                               : run_grad<f16>(*q, p, (char *)d_ws, (hipStream_t)stream);
