@@ -64,17 +64,17 @@ __device__ inline f32x4 unpack_e4m3(unsigned w) {
 }
 
 __device__ inline unsigned load_codes(const unsigned char *p, int valid) {
-    if (valid >= 4) return reinterpret_cast<const Loose<unsigned, 1> *>(p)->v;
+    if (valid >= 4) return __builtin_nontemporal_load(&((const Global<Loose<unsigned, 1>> *)p)->v);
     unsigned w = 0;
-    for (int e = 0; e < valid; ++e) w |= (unsigned)p[e] << (8 * e);
+    for (int e = 0; e < valid; ++e) w |= (unsigned)((const Global<unsigned char> *)p)[e] << (8 * e);
     return w;
 }
 __device__ inline void store_codes(unsigned char *p, unsigned w, int valid) {
     if (valid >= 4) {
-        reinterpret_cast<Loose<unsigned, 1> *>(p)->v = w;
+        __builtin_nontemporal_store(w, &((Global<Loose<unsigned, 1>> *)p)->v);
         return;
     }
-    for (int e = 0; e < valid; ++e) p[e] = (unsigned char)(w >> (8 * e));
+    for (int e = 0; e < valid; ++e) ((Global<unsigned char> *)p)[e] = (unsigned char)(w >> (8 * e));
 }
 
 // The block's values over their scale, rounded at random; lane 0 has the scale.
@@ -116,18 +116,18 @@ __global__ __launch_bounds__(256) void adamw_kernel(const tg_adamw_tensor *__res
         const int64_t at = base + s * kScaleBlock + lane * 4;
         const int64_t left = t.n - at;
         valid[s] = left >= 4 ? 4 : left > 0 ? (int)left : 0;
-        g[s] = load_f32<G, 4>(grad + at, valid[s]);
-        w[s] = kMaster ? load_f32<float, 4>(t.master + at, valid[s]) : load_f32<P, 4>(param + at, valid[s]);
+        g[s] = load_f32<G, 4, true>(grad + at, valid[s]);
+        w[s] = kMaster ? load_f32<float, 4, true>(t.master + at, valid[s]) : load_f32<P, 4, true>(param + at, valid[s]);
         if (kEight) {
             mc[s] = load_codes((const unsigned char *)t.m + at, valid[s]);
             vc[s] = load_codes((const unsigned char *)t.v + at, valid[s]);
             const bool any = base + s * kScaleBlock < t.n;
             const int64_t block = base / kScaleBlock + s;
-            ms[s] = any ? t.m_scale[block] : 0.0f;
-            vs[s] = any ? t.v_scale[block] : 0.0f;
+            ms[s] = any ? ((const Global<float> *)t.m_scale)[block] : 0.0f;
+            vs[s] = any ? ((const Global<float> *)t.v_scale)[block] : 0.0f;
         } else {
-            m[s] = load_f32<float, 4>((const float *)t.m + at, valid[s]);
-            v[s] = load_f32<float, 4>((const float *)t.v + at, valid[s]);
+            m[s] = load_f32<float, 4, true>((const float *)t.m + at, valid[s]);
+            v[s] = load_f32<float, 4, true>((const float *)t.v + at, valid[s]);
         }
     }
     const unsigned key = kEight ? mix(r.key + (unsigned)c.tensor * 0x13198A2Fu) : 0u;
@@ -152,12 +152,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(const tg_adamw_tensor *__res
             // bits then do to an 8-bit moment can be recomputed anywhere
             m[s][e] = r.beta1 * m[s][e] + r.one_minus_beta1 * ge;
             v[s][e] = r.beta2 * v[s][e] + r.one_minus_beta2 * ge * ge;
-            root[e] = sqrtf(v[s][e]);
-            const float step = (r.lr_over_c1 * m[s][e]) / fmaf(root[e], r.rsqrt_c2, r.eps);
+            root[e] = kEight ? sqrtf(v[s][e]) : __builtin_amdgcn_sqrtf(v[s][e]);
+            const float step = r.lr_over_c1 * m[s][e] * __builtin_amdgcn_rcpf(fmaf(root[e], r.rsqrt_c2, r.eps));
             w[s][e] -= fmaf(r.decay, w[s][e], step);
         }
-        if (kMaster) store_f32<float, 4>(t.master + at, w[s], valid[s]);
-        store_f32<P, 4>(param + at, w[s], valid[s]);
+        if (kMaster) store_f32<float, 4, true>(t.master + at, w[s], valid[s]);
+        store_f32<P, 4, true>(param + at, w[s], valid[s]);
         if (kEight) {
             unsigned bm[4], bv[4];
 #pragma unroll
@@ -172,12 +172,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(const tg_adamw_tensor *__res
             store_codes((unsigned char *)t.m + at, qm, valid[s]);
             store_codes((unsigned char *)t.v + at, qv, valid[s]);
             if (lane == 0) {
-                t.m_scale[base / kScaleBlock + s] = m_scale;
-                t.v_scale[base / kScaleBlock + s] = v_scale;
+                ((Global<float> *)t.m_scale)[base / kScaleBlock + s] = m_scale;
+                ((Global<float> *)t.v_scale)[base / kScaleBlock + s] = v_scale;
             }
         } else {
-            store_f32<float, 4>((float *)t.m + at, m[s], valid[s]);
-            store_f32<float, 4>((float *)t.v + at, v[s], valid[s]);
+            store_f32<float, 4, true>((float *)t.m + at, m[s], valid[s]);
+            store_f32<float, 4, true>((float *)t.v + at, v[s], valid[s]);
         }
     }
 }

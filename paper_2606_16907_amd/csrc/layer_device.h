@@ -30,40 +30,54 @@ template <typename V, int A>
 struct __attribute__((packed, aligned(A))) Loose {
     V v;
 };
-template <typename T, int N>
+// Operands lie in device memory, which the compiler does not know of addresses
+// that come out of a table.
+template <typename T>
+using Global = __attribute__((address_space(1))) T;
+
+// kOnce: what is read or written once in a pass much larger than the caches need
+// not stay in them.
+template <typename T, int N, bool kOnce = false>
 __device__ inline vec<T, N> load_loose(const T *p) {
-    return reinterpret_cast<const Loose<vec<T, N>, alignof(T)> *>(p)->v;
+    const auto *const at = &((const Global<Loose<vec<T, N>, alignof(T)>> *)p)->v;
+    return kOnce ? __builtin_nontemporal_load(at) : *at;
 }
-template <typename T, int N>
+template <typename T, int N, bool kOnce = false>
 __device__ inline void store_loose(T *p, vec<T, N> v) {
-    reinterpret_cast<Loose<vec<T, N>, alignof(T)> *>(p)->v = v;
+    auto *const at = &((Global<Loose<vec<T, N>, alignof(T)>> *)p)->v;
+    if (kOnce)
+        __builtin_nontemporal_store(v, at);
+    else
+        *at = v;
 }
 
 // N elements of p as floats; those at or past `valid` are 0 and not read.
-template <typename T, int N>
+template <typename T, int N, bool kOnce = false>
 __device__ inline vec<float, N> load_f32(const T *p, int valid) {
     vec<float, N> r;
     if (valid >= N) {
-        const vec<T, N> v = load_loose<T, N>(p);
+        const vec<T, N> v = load_loose<T, N, kOnce>(p);
 #pragma unroll
         for (int e = 0; e < N; ++e) r[e] = (float)v[e];
     } else {
+        const Global<T> *const g = (const Global<T> *)p;
 #pragma unroll
-        for (int e = 0; e < N; ++e) r[e] = e < valid ? (float)p[e] : 0.0f;
+        for (int e = 0; e < N; ++e) r[e] = e < valid ? (float)g[e] : 0.0f;
     }
     return r;
 }
-template <typename T, int N>
+template <typename T, int N, bool kOnce = false>
 __device__ inline void store_f32(T *p, vec<float, N> r, int valid) {
     if (valid >= N) {
         vec<T, N> v;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (T)r[e];
-        store_loose<T, N>(p, v);
+        store_loose<T, N, kOnce>(p, v);
     } else {
+        Global<T> *const g = (Global<T> *)p;
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            if (e < valid) p[e] = (T)r[e];
+            if (e < valid) g[e] = (T)r[e];
     }
 }
 
@@ -80,12 +94,22 @@ struct OpMax {
     static __device__ float of(float a, float b) { return fmaxf(a, b); }
 };
 
-// All lanes get the reduction over the wave, in a fixed order.
+// All lanes get the reduction over the wave, in a fixed order: within rows of 16
+// lanes by their data-parallel moves, then across rows by swapping them.
+template <int kMove>
+__device__ inline float moved(float x) {
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kMove, 0xf, 0xf, true));
+}
 template <typename Op>
 __device__ inline float wave_reduce(float x) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x = Op::of(x, __shfl_xor(x, d));
-    return x;
+    x = Op::of(x, moved<0xB1>(x));   // neighbours
+    x = Op::of(x, moved<0x4E>(x));   // pairs of four
+    x = Op::of(x, moved<0x141>(x));  // fours of eight, mirrored
+    x = Op::of(x, moved<0x140>(x));  // eights of sixteen, mirrored
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = Op::of(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return Op::of(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
 }
 // All threads of a block of T get the reduction; T = 64 is the wave alone.
 // `slots` holds T / 64 floats and is free again when the next use begins after

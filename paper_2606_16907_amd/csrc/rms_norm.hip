@@ -4,7 +4,7 @@
 // Both are bound by memory: forward reads x and residual and writes hidden and
 // y, backward reads dy, hidden and dhidden and writes dx, each once, so a row
 // stays in registers between its statistic and its output.  A row is cut into
-// units of 8 elements; thread t of the row's T threads holds units t, t + T, ...
+// units of 16 bytes; thread t of the row's T threads holds units t, t + T, ...
 // (N of them), every load of the row in flight before the reduction.
 #include <algorithm>
 #include <cmath>
@@ -14,8 +14,8 @@
 namespace tg {
 namespace {
 
-constexpr int kUnit = 8;
-using f32x8 = vec<float, 8>;
+template <typename E>
+constexpr int kUnitOf = 16 / sizeof(E);
 
 struct NormArgs {
     const void *x, *residual, *weight;
@@ -29,15 +29,16 @@ struct NormArgs {
 
 __device__ inline int left_of(int cols, int col) { return cols - col; }  // <= 0: none
 
-__device__ inline void store_e4m3(unsigned char *p, f32x8 q, int valid) {
-    unsigned w[2];
+template <int kUnit>
+__device__ inline void store_e4m3(unsigned char *p, vec<float, kUnit> q, int valid) {
+    vec<unsigned, kUnit / 4> w;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kUnit / 4; ++h) {
         int t = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], 0, false);
         w[h] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], t, true);
     }
     if (valid >= kUnit) {
-        reinterpret_cast<Loose<vec<unsigned, 2>, 1> *>(p)->v = vec<unsigned, 2>{w[0], w[1]};
+        reinterpret_cast<Loose<vec<unsigned, kUnit / 4>, 1> *>(p)->v = w;
     } else {
 #pragma unroll
         for (int e = 0; e < kUnit; ++e)
@@ -45,11 +46,13 @@ __device__ inline void store_e4m3(unsigned char *p, f32x8 q, int valid) {
     }
 }
 
-// One row per T threads, N units a thread (8 T N >= cols), 256 / T rows a block
+// One row per T threads, N units a thread (T N units or more), 256 / T rows a block
 // where T is 64.  kStream: rows of any length, read again for each pass (x and
 // residual add up to the same h every time), one row a block.
 template <typename E, bool kEight, int T, int N, bool kStream>
 __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
     constexpr int kRows = T == 64 ? 4 : 1;
     __shared__ float slots[2][T / 64];
     const int t = threadIdx.x % T;
@@ -62,22 +65,22 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
 
     const auto read = [&](int col) {
         const int valid = left_of(a.cols, col);
-        f32x8 h = load_f32<E, kUnit>(x + col, valid);
+        unit h = load_f32<E, kUnit>(x + col, valid);
         if (r) h += load_f32<E, kUnit>(r + col, valid);
         return h;
     };
-    const auto write = [&](int col, f32x8 y, float scale) {
+    const auto write = [&](int col, unit y, float scale) {
         const int valid = left_of(a.cols, col);
         if (kEight) {
 #pragma unroll
             for (int e = 0; e < kUnit; ++e) y[e] /= scale;
-            store_e4m3((unsigned char *)a.y + row * a.ldy + col, y, valid);
+            store_e4m3<kUnit>((unsigned char *)a.y + row * a.ldy + col, y, valid);
         } else {
             store_f32<E, kUnit>((E *)a.y + row * a.ldy + col, y, valid);
         }
     };
 
-    f32x8 h[N];
+    unit h[N];
     float squares = 0.0f;
     const int units = (a.cols + kUnit - 1) / kUnit;
     if (kStream) {
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
         }
     } else {
 #pragma unroll
-        for (int n = 0; n < N; ++n) h[n] = t + n * T < units ? read((t + n * T) * kUnit) : f32x8(0.0f);
+        for (int n = 0; n < N; ++n) h[n] = t + n * T < units ? read((t + n * T) * kUnit) : unit(0.0f);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
 #pragma unroll
@@ -99,9 +102,9 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
     const float rstd = 1.0f / sqrtf(fmaf(squares, a.inv_cols, a.eps));
     if (a.rstd && t == 0) a.rstd[row] = rstd;
 
-    const auto normed = [&](f32x8 v, int col) {
-        const f32x8 w = load_f32<E, kUnit>(weight + col, left_of(a.cols, col));
-        f32x8 y;
+    const auto normed = [&](unit v, int col) {
+        const unit w = load_f32<E, kUnit>(weight + col, left_of(a.cols, col));
+        unit y;
 #pragma unroll
         for (int e = 0; e < kUnit; ++e) y[e] = (v[e] * rstd) * w[e];
         return y;
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
         float most = 0.0f;
         if (kStream) {
             for (int u = t; u < units; u += T) {
-                const f32x8 y = normed(read(u * kUnit), u * kUnit);
+                const unit y = normed(read(u * kUnit), u * kUnit);
 #pragma unroll
                 for (int e = 0; e < kUnit; ++e) most = fmaxf(most, finite_abs(y[e]));
             }
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
     }
     if (kStream) {
         for (int u = t; u < units; u += T) {
-            const f32x8 v = read(u * kUnit);
+            const unit v = read(u * kUnit);
             // hidden may be x or residual: this unit was just read for the last time
             if (hidden) store_f32<E, kUnit>(hidden + u * kUnit, v, left_of(a.cols, u * kUnit));
             write(u * kUnit, normed(v, u * kUnit), scale);
@@ -164,18 +167,20 @@ struct GradArgs {
 // of dweight in registers over all of them; one row of sums a block leaves it.
 template <typename E, int T, int N>
 __global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
     __shared__ float slots[2][T / 64];
     const int t = threadIdx.x;
     const int units = (a.cols + kUnit - 1) / kUnit;
     constexpr bool kKeep = T < 1024;
-    f32x8 kept[N], dw[N];
+    unit kept[N], dw[N];
     const auto weight = [&](int n) {
         const int u = t + n * T;
-        return u < units ? load_f32<E, kUnit>((const E *)a.weight + u * kUnit, left_of(a.cols, u * kUnit)) : f32x8(0.0f);
+        return u < units ? load_f32<E, kUnit>((const E *)a.weight + u * kUnit, left_of(a.cols, u * kUnit)) : unit(0.0f);
     };
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        dw[n] = f32x8(0.0f);
+        dw[n] = unit(0.0f);
         if (kKeep) kept[n] = weight(n);
     }
     int turn = 0;
@@ -183,11 +188,11 @@ __global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
         const E *const dy = (const E *)a.dy + row * a.lddy;
         const E *const hidden = (const E *)a.hidden + row * a.ldh;
         const E *const dh = a.dhidden ? (const E *)a.dhidden + row * a.lddh : nullptr;
-        f32x8 g[N], h[N], more[N];
+        unit g[N], h[N], more[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int u = t + n * T, valid = u < units ? left_of(a.cols, u * kUnit) : 0;
-            g[n] = h[n] = more[n] = f32x8(0.0f);
+            g[n] = h[n] = more[n] = unit(0.0f);
             if (u >= units) continue;
             g[n] = load_f32<E, kUnit>(dy + u * kUnit, valid);
             h[n] = load_f32<E, kUnit>(hidden + u * kUnit, valid);
@@ -197,7 +202,7 @@ __global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
         float dot = 0.0f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const f32x8 w = kKeep ? kept[n] : weight(n);
+            const unit w = kKeep ? kept[n] : weight(n);
 #pragma unroll
             for (int e = 0; e < kUnit; ++e) {
                 const float xhat = h[n][e] * rstd;
@@ -214,7 +219,7 @@ __global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
         for (int n = 0; n < N; ++n) {
             const int u = t + n * T;
             if (u >= units) continue;
-            f32x8 d;
+            unit d;
 #pragma unroll
             for (int e = 0; e < kUnit; ++e) d[e] = fmaf(rstd, fmaf(-h[n][e], mean, g[n][e]), more[n][e]);
             store_f32<E, kUnit>(dx + u * kUnit, d, left_of(a.cols, u * kUnit));
@@ -232,13 +237,15 @@ __global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
 // be dy), a thread a unit of columns and a block a share of the rows ...
 template <typename E>
 __global__ __launch_bounds__(256) void norm_grad_weight_stream(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
     const int u = blockIdx.y * 256 + threadIdx.x;
     if (u * (int64_t)kUnit >= a.cols) return;
     const int col = u * kUnit, valid = left_of(a.cols, col);
-    f32x8 dw(0.0f);
+    unit dw(0.0f);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const f32x8 g = load_f32<E, kUnit>((const E *)a.dy + row * a.lddy + col, valid);
-        const f32x8 h = load_f32<E, kUnit>((const E *)a.hidden + row * a.ldh + col, valid);
+        const unit g = load_f32<E, kUnit>((const E *)a.dy + row * a.lddy + col, valid);
+        const unit h = load_f32<E, kUnit>((const E *)a.hidden + row * a.ldh + col, valid);
         const float rstd = a.rstd[row];
 #pragma unroll
         for (int e = 0; e < kUnit; ++e) dw[e] = fmaf(g[e], h[e] * rstd, dw[e]);
@@ -248,6 +255,8 @@ __global__ __launch_bounds__(256) void norm_grad_weight_stream(GradArgs a) {
 // ... then dx, a row a block, read twice.
 template <typename E>
 __global__ __launch_bounds__(1024) void norm_grad_stream(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
     __shared__ float slots[16];
     const int64_t row = a.first + blockIdx.x;
     const int units = (a.cols + kUnit - 1) / kUnit;
@@ -259,17 +268,17 @@ __global__ __launch_bounds__(1024) void norm_grad_stream(GradArgs a) {
     float dot = 0.0f;
     for (int u = threadIdx.x; u < units; u += 1024) {
         const int col = u * kUnit, valid = left_of(a.cols, col);
-        const f32x8 g = load_f32<E, kUnit>(dy + col, valid), h = load_f32<E, kUnit>(hidden + col, valid);
-        const f32x8 w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
+        const unit g = load_f32<E, kUnit>(dy + col, valid), h = load_f32<E, kUnit>(hidden + col, valid);
+        const unit w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
 #pragma unroll
         for (int e = 0; e < kUnit; ++e) dot = fmaf(g[e] * w[e], h[e] * rstd, dot);
     }
     const float mean = block_reduce<OpSum, 1024>(dot, slots) * a.inv_cols;
     for (int u = threadIdx.x; u < units; u += 1024) {
         const int col = u * kUnit, valid = left_of(a.cols, col);
-        const f32x8 g = load_f32<E, kUnit>(dy + col, valid), h = load_f32<E, kUnit>(hidden + col, valid);
-        const f32x8 w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
-        f32x8 d(0.0f);
+        const unit g = load_f32<E, kUnit>(dy + col, valid), h = load_f32<E, kUnit>(hidden + col, valid);
+        const unit w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
+        unit d(0.0f);
         if (dh) d = load_f32<E, kUnit>(dh + col, valid);
 #pragma unroll
         for (int e = 0; e < kUnit; ++e) d[e] = fmaf(rstd, fmaf(-(h[e] * rstd), mean, g[e] * w[e]), d[e]);
@@ -281,7 +290,7 @@ constexpr int64_t kMostBlocks = 1 << 20;  // of a launch: a grid holds fewer tha
 
 template <typename E, bool kEight>
 hipError_t launch_norm(NormArgs a, hipStream_t s) {
-    const int units = (a.cols + kUnit - 1) / kUnit;
+    const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
     const auto go = [&](auto kernel, int threads, int rows_per_block) {
         for (a.first = 0; a.first < a.rows; a.first += kMostBlocks * rows_per_block) {
             const int64_t blocks = std::min(kMostBlocks, ceil_div(a.rows - a.first, rows_per_block));
@@ -318,20 +327,23 @@ int grad_blocks(int64_t rows) { return (int)(rows < 512 ? rows : 512); }
 
 template <typename E>
 hipError_t launch_grad(GradArgs a, hipStream_t s) {
-    const int units = (a.cols + kUnit - 1) / kUnit;
+    const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
     const dim3 grid((unsigned)grad_blocks(a.rows));
     const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a); };
-    if (units <= 64)
+    constexpr int kMost = kUnitOf<E> == 4 ? 4096 : 2048;  // units of a row that stays in registers
+    if (units <= 64) {
         go(norm_grad_kernel<E, 64, 1>, 64);
-    else if (units <= 256)
+    } else if (units <= 256) {
         go(norm_grad_kernel<E, 256, 1>, 256);
-    else if (units <= 512)
+    } else if (units <= 512) {
         go(norm_grad_kernel<E, 256, 2>, 256);
-    else if (units <= 1024)
+    } else if (units <= 1024) {
         go(norm_grad_kernel<E, 512, 2>, 512);
-    else if (units <= 2048)
+    } else if (units <= 2048) {
         go(norm_grad_kernel<E, 1024, 2>, 1024);
-    else {
+    } else if (units <= kMost) {
+        go(norm_grad_kernel<E, 1024, kMost / 1024>, 1024);
+    } else {
         hipLaunchKernelGGL(norm_grad_weight_stream<E>, dim3(grid.x, (unsigned)ceil_div(units, 256)), dim3(256), 0, s, a);
         for (; a.first < a.rows; a.first += kMostBlocks)
             hipLaunchKernelGGL(norm_grad_stream<E>, dim3((unsigned)std::min(kMostBlocks, a.rows - a.first)), dim3(1024), 0, s, a);
