@@ -584,12 +584,12 @@ constexpr int64_t kMostLd = 1 << 21;  // elements of a row of a product's operan
 
 // How a product is cut: tiles of 256 or 128, and r into splits, whichever is
 // estimated to take the least time.  Measured, in us: a step of a 256 tile takes
-// 1.35 while few of the 256 CUs work and 1.8 when all do (8192^3: 1.75), one of a
-// 128 tile 0.65 alone on its CU and 1.05 beside another; beginning and end of a
-// tile take 9 and 3; the shares of a split are written and read at 4 TB/s, in a
-// launch of 3.  2048 x 1024 x 4096: 24 in tiles of 128 and 38 of 256;
-// 8192 x 8192 x 8192: 862 of 256 and 1010 of 128; its gradient with sums of 4096
-// over 2048 x 1024: 42 unsplit, 33 in two.
+// 1.05 while few of the 256 CUs work and 1.58 when all do, one of a 128 tile 0.38
+// to 0.56 alone on its CU and 0.95 beside another; beginning and end of a tile
+// take 9 and 3 to 5; the shares of a split are written and read at 4 TB/s, in a
+// launch of 3.  2048 x 1024 x 4096: 24 in tiles of 128 and 36 of 256; 4096^3: 125
+// of 128 and 110 of 256; its gradient with sums of 4096 over 2048 x 1024: 34
+// unsplit, 29 in two.  Tiles of 256 x 128 were within 5% of the better of the two.
 struct Cut {
     int tile, splits, share;  // share: steps of a split
 };
@@ -602,11 +602,12 @@ Cut cut_product(int64_t ni, int64_t nj, int64_t nr, int size) {
             const int share = want == 1 ? (int)steps : (int)(ceil_div(ceil_div(steps, want), 2) * 2);
             const int splits = (int)ceil_div(steps, share);
             const int64_t blocks = ceil_div(ni, tile) * ceil_div(nj, tile) * splits;
+            const double used = std::min(1.0, blocks / 256.0);
             double us;
             if (tile == 256)
-                us = ceil_div(blocks, 256) * (9 + share * (blocks < 256 ? 1.35 + 0.45 * blocks / 256 : 1.8));
+                us = ceil_div(blocks, 256) * (9 + share * (1.05 + 0.53 * used));
             else
-                us = blocks <= 256 ? 3 + share * 0.65 : ceil_div(blocks, 512) * (3 + share * 1.05);
+                us = blocks <= 256 ? 3 + share * (0.33 + 0.23 * used) : ceil_div(blocks, 512) * (5 + share * 0.95);
             if (splits > 1) us += 3 + splits * (double)ni * nj * 8 / 4e6;
             if (least == 0 || us < least) least = us, best = Cut{tile, splits, share};
         }

@@ -309,7 +309,7 @@ hipError_t launch_norm(NormArgs a, hipStream_t s) {
     else if (units <= 512 && a.rows >= 256)
         go(norm_kernel<E, kEight, 256, 2, false>, 256, 1);
     else if (units <= 1024 && a.rows >= 256)
-        go(norm_kernel<E, kEight, 256, 4, false>, 256, 1);
+        go(norm_kernel<E, kEight, 512, 2, false>, 512, 1);
     else if (units <= 1024)
         go(norm_kernel<E, kEight, 1024, 1, false>, 1024, 1);
     else if (units <= 2048)
