@@ -51,7 +51,17 @@ __device__ inline void store_loose(T *p, vec<T, N> v) {
         *at = v;
 }
 
-// N elements of p as floats; those at or past `valid` are 0 and not read.
+// N elements of p; those at or past `valid` are 0 and not read.
+template <typename T, int N>
+__device__ inline vec<T, N> load_part(const T *p, int valid) {
+    if (valid >= N) return load_loose<T, N>(p);
+    vec<T, N> r;
+    const Global<T> *const g = (const Global<T> *)p;
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = e < valid ? g[e] : (T)0.0f;
+    return r;
+}
+// The same as floats.
 template <typename T, int N, bool kOnce = false>
 __device__ inline vec<float, N> load_f32(const T *p, int valid) {
     vec<float, N> r;

@@ -102,18 +102,34 @@ __device__ inline vec<float, N> slope(vec<float, N> z, int act) {
     return z;
 }
 
-// N columns from j on of row i.
+// N columns from j on of row i, from the sums z and what the row's and the columns'
+// operands are: sx the row's scale, sw the columns', `residual` theirs.
+template <int N>
+struct Columns {
+    vec<float, N> sw, bias;
+};
 template <typename O, int N>
-__device__ inline void finish(vec<float, N> z, int64_t i, int64_t j, int valid, const Epilogue &e) {
-    if (e.x_scale) {
-        z *= e.x_scale[i];
-        z *= load_f32<float, N>(e.w_scale + j, valid);
-    }
-    if (e.bias) z += load_f32<O, N>((const O *)e.bias + j, valid);
+__device__ inline Columns<N> load_columns(int64_t j, int valid, const Epilogue &e) {
+    Columns<N> c{vec<float, N>(1.0f), vec<float, N>(0.0f)};
+    if (e.w_scale) c.sw = load_f32<float, N>(e.w_scale + j, valid);
+    if (e.bias) c.bias = load_f32<O, N>((const O *)e.bias + j, valid);
+    return c;
+}
+template <typename O, int N>
+__device__ inline void finish(vec<float, N> z, float sx, const Columns<N> &c, vec<float, N> residual, int64_t i, int64_t j, int valid,
+                              const Epilogue &e) {
+    if (e.x_scale) z = z * sx * c.sw;
+    z += c.bias;
     if (e.pre) store_f32<O, N>((O *)e.pre + i * e.ldp + j, z, valid);
     activate<N>(z, e.act);
-    if (e.residual) z += load_f32<O, N>((const O *)e.residual + i * e.ldr + j, valid);
+    if (e.residual) z += residual;
     store_f32<O, N>((O *)e.out + i * e.ldo + j, z, valid);
+}
+template <typename O, int N>
+__device__ inline void finish(vec<float, N> z, int64_t i, int64_t j, int valid, const Epilogue &e) {
+    vec<float, N> residual(0.0f);
+    if (e.residual) residual = load_f32<O, N>((const O *)e.residual + i * e.ldr + j, valid);
+    finish<O, N>(z, e.x_scale ? e.x_scale[i] : 1.0f, load_columns<O, N>(j, valid, e), residual, i, j, valid, e);
 }
 
 // ---------------------------------------------------------------------------
@@ -468,9 +484,37 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     // each 32 x 32 part.  32 rows at a time go through the wave's share of LDS, in
     // rows 16 bytes longer than their values so that the rows of a column meet
     // different banks, and come back 8 columns a lane, whole rows side by side.
+    // The residual's units and the rows' scales of the next 32 rows are on their way
+    // meanwhile, and wait beside the sums: the loop over a lane's units is not
+    // unrolled, so that the activations' code stays small.
     __syncthreads();
-    constexpr int kRow = 32 * kTJ + 4;
-    float *const rows = (float *)&tiles[0] + wave * 32 * kRow;
+    constexpr int kRow = 32 * kTJ + 4, kUnits = 2 * kTJ, kShare = 32 * kRow * 4 + 32 * 32 * kTJ * 2 + 128;
+    static_assert(4 * kShare <= (int)sizeof(tiles), "the waves' shares fit the tiles' place");
+    float *const rows = (float *)(&tiles[0] + wave * kShare);
+    vec<O, 8> *const kept = (vec<O, 8> *)(rows + 32 * kRow);
+    float *const scales = (float *)(kept + 32 * 4 * kTJ);
+    const int col = lane % (4 * kTJ) * 8;  // the same in all of a lane's units
+    const int64_t j = j0 + wj + col;
+    const int valid = (int)std::min<int64_t>(8, a.nj - j);
+    Columns<8> columns{};
+    vec<O, 8> fetched[kUnits];
+    float scale = 1.0f;
+    const auto row_of = [&](int x, int n) { return i0 + wi + x * 32 + n * (64 / (4 * kTJ)) + lane / (4 * kTJ); };
+    const auto fetch = [&](int x) {
+        if (e.residual) {
+#pragma unroll
+            for (int n = 0; n < kUnits; ++n) {
+                const int64_t i = row_of(x, n);
+                fetched[n] = load_part<O, 8>((const O *)e.residual + i * e.ldr + j, i < a.ni ? valid : 0);
+            }
+        }
+        const int64_t i = i0 + wi + x * 32 + lane % 32;
+        if (e.x_scale) scale = i < a.ni ? e.x_scale[i] : 1.0f;
+    };
+    if (!e.partial) {
+        if (valid > 0) columns = load_columns<O, 8>(j, valid, e);
+        fetch(0);
+    }
 #pragma unroll
     for (int x = 0; x < kTI; ++x) {
 #pragma unroll
@@ -481,19 +525,29 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
                 *(f32x4 *)(rows + (lane % 32) * kRow + y * 32 + 2 * c + (lane / 32) * 4) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
             }
         }
+        if (!e.partial) {
+            if (e.residual) {
+#pragma unroll
+                for (int n = 0; n < kUnits; ++n) kept[n * 64 + lane] = fetched[n];
+            }
+            if (e.x_scale && lane < 32) scales[lane] = scale;
+            if (x + 1 < kTI) fetch(x + 1);
+        }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-        for (int u = lane; u < 32 * 4 * kTJ; u += 64) {
-            const int row = u / (4 * kTJ), col = u % (4 * kTJ) * 8;
-            const int64_t i = i0 + wi + x * 32 + row, j = j0 + wj + col;
-            if (i >= a.ni || j >= a.nj) continue;
+        for (int n = 0; n < kUnits; ++n) {
+            const int64_t i = row_of(x, n);
+            if (i >= a.ni || valid <= 0) continue;
+            const int row = (int)(i - i0 - wi) - x * 32;
             const f32x4 lo = *(const f32x4 *)(rows + row * kRow + col), hi = *(const f32x4 *)(rows + row * kRow + col + 4);
             const vec<float, 8> z = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            const int valid = (int)std::min<int64_t>(8, a.nj - j);
-            if (e.partial)
+            if (e.partial) {
                 store_f32<float, 8>(e.partial + (blockIdx.y * a.ni + i) * a.nj + j, z, valid);
-            else
-                finish<O, 8>(z, i, j, valid, e);
+                continue;
+            }
+            vec<float, 8> residual(0.0f);
+            if (e.residual) residual = __builtin_convertvector(kept[n * 64 + lane], vec<float, 8>);
+            finish<O, 8>(z, e.x_scale ? scales[row] : 1.0f, columns, residual, i, j, valid, e);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -586,8 +640,8 @@ constexpr int64_t kMostLd = 1 << 21;  // elements of a row of a product's operan
 // estimated to take the least time.  Measured, in us: a step of a 256 tile takes
 // 1.05 while few of the 256 CUs work and 1.58 when all do, one of a 128 tile 0.38
 // to 0.56 alone on its CU and 0.95 beside another; beginning and end of a tile
-// take 9 and 3 to 5; the shares of a split are written and read at 4 TB/s, in a
-// launch of 3.  2048 x 1024 x 4096: 24 in tiles of 128 and 36 of 256; 4096^3: 125
+// take 9 and 3 to 5; the shares of a split are written and read at 4 TB/s, at 8
+// while the caches hold them, in a launch of 3.  2048 x 1024 x 4096: 24 in tiles of 128 and 36 of 256; 4096^3: 125
 // of 128 and 110 of 256; its gradient with sums of 4096 over 2048 x 1024: 34
 // unsplit, 29 in two.  Tiles of 256 x 128 were within 5% of the better of the two.
 struct Cut {
@@ -608,7 +662,8 @@ Cut cut_product(int64_t ni, int64_t nj, int64_t nr, int size) {
                 us = ceil_div(blocks, 256) * (9 + share * (1.05 + 0.53 * used));
             else
                 us = blocks <= 256 ? 3 + share * (0.33 + 0.23 * used) : ceil_div(blocks, 512) * (5 + share * 0.95);
-            if (splits > 1) us += 3 + splits * (double)ni * nj * 8 / 4e6;
+            const double moved = splits * (double)ni * nj * 8;
+            if (splits > 1) us += 3 + moved / (moved < 64e6 ? 8e6 : 4e6);
             if (least == 0 || us < least) least = us, best = Cut{tile, splits, share};
         }
     }
