@@ -131,12 +131,19 @@ def _act(act):
     return ACTS[act]
 
 
-def _out(out, like, m, n, dtype, device):
+def _out(out, like, m, n, dtype, device, what="out"):
     """The [m, n] output, its pointer and row stride."""
     if out is None:
         out = like.new_empty((m, n), dtype=dtype)
         return out, out.data_ptr(), n
-    return out, *_matrix(out, dtype, m, n, "out", device)
+    return out, *_matrix(out, dtype, m, n, what, device)
+
+
+def _vector_out(out, like, n, device, what):
+    if out is None:
+        out = like.new_empty(n)
+        return out, out.data_ptr()
+    return out, _vector(out, like.dtype, n, what, device)
 
 
 def tg_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=None, out_dtype=None,
@@ -176,10 +183,11 @@ def tg_linear(x, w, bias=None, act="none", residual=None, x_scale=None, w_scale=
     return (y, pre) if keep_pre else y
 
 
-def tg_linear_grad(dy, x, w, pre=None, act="none", bias_grad=False, x_grad=True, w_grad=True, workspace=None):
+def tg_linear_grad(dy, x, w, pre=None, act="none", bias_grad=False, x_grad=True, w_grad=True, dx=None, dw=None,
+                   dbias=None, workspace=None):
     """(dx, dw, dbias) of tg_linear from dy [m, n], in the inputs' type; those
-    not asked for are None.  The residual's gradient is dy.  `pre` is
-    tg_linear's, needed where there is an activation."""
+    not asked for are None, those given are written to.  The residual's gradient
+    is dy.  `pre` is tg_linear's, needed where there is an activation."""
     lib = load_library()
     device = torch.cuda.current_device()
     dtype = dy.dtype
@@ -194,11 +202,10 @@ def tg_linear_grad(dy, x, w, pre=None, act="none", bias_grad=False, x_grad=True,
     if act and pre is None:
         raise ValueError("pre: needed for the gradient of an activation (tg_linear with keep_pre)")
     pp, ldp = _matrix(pre, dtype, m, n, "pre", device) if act else (None, 0)
-    dx, pdx, lddx = _out(None, dy, m, k, dtype, device) if x_grad else (None, None, 0)
-    dw, pdw, lddw = _out(None, dy, n, k, dtype, device) if w_grad else (None, None, 0)
-    db = dy.new_empty(n) if bias_grad else None
-    a = TgLinearGradArgs(pdy, pp, px, pw, pdx, pdw, None if db is None else db.data_ptr(), m, n, k, lddy, ldp, ldx, ldw,
-                         lddx, lddw, TYPES[dtype], act)
+    dx, pdx, lddx = _out(dx, dy, m, k, dtype, device, "dx") if x_grad else (None, None, 0)
+    dw, pdw, lddw = _out(dw, dy, n, k, dtype, device, "dw") if w_grad else (None, None, 0)
+    db, pdb = _vector_out(dbias, dy, n, device, "dbias") if bias_grad else (None, None)
+    a = TgLinearGradArgs(pdy, pp, px, pw, pdx, pdw, pdb, m, n, k, lddy, ldp, ldx, ldw, lddx, lddw, TYPES[dtype], act)
     ws, size, _kept = _workspace(lib.tg_linear_grad_workspace_bytes(a), workspace, dy, device)
     T._check(lib.tg_linear_grad(a, ws, size, _stream(device)), "tg_linear_grad")
     return dx, dw, db
@@ -241,9 +248,10 @@ def tg_rms_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, out=None, ke
     return Norm(y, scale, hidden, rstd)
 
 
-def tg_rms_norm_grad(dy, hidden, weight, rstd, dhidden=None, workspace=None):
+def tg_rms_norm_grad(dy, hidden, weight, rstd, dhidden=None, dx=None, dweight=None, workspace=None):
     """(dx, dweight) of tg_rms_norm; dx is the gradient of x and of the residual
-    alike.  dhidden is the gradient that arrives at `hidden` from further on."""
+    alike.  dhidden is the gradient that arrives at `hidden` from further on; dx
+    and dweight are written to where they are given (dx may be dy or dhidden)."""
     lib = load_library()
     device = torch.cuda.current_device()
     dtype = dy.dtype
@@ -255,9 +263,9 @@ def tg_rms_norm_grad(dy, hidden, weight, rstd, dhidden=None, workspace=None):
     pw = _vector(weight, dtype, cols, "weight", device)
     ps = _vector(rstd, torch.float32, rows, "rstd", device)
     pdh, lddh = (None, 0) if dhidden is None else _matrix(dhidden, dtype, rows, cols, "dhidden", device)
-    dx, pdx, lddx = _out(None, dy, rows, cols, dtype, device)
-    dweight = dy.new_empty(cols)
-    a = TgRmsNormGradArgs(pdy, pdh, ph, pw, ps, pdx, dweight.data_ptr(), rows, cols, lddy, lddh, ldh, lddx,
+    dx, pdx, lddx = _out(dx, dy, rows, cols, dtype, device, "dx")
+    dweight, pdw = _vector_out(dweight, dy, cols, device, "dweight")
+    a = TgRmsNormGradArgs(pdy, pdh, ph, pw, ps, pdx, pdw, rows, cols, lddy, lddh, ldh, lddx,
                           TYPES[dtype], 0)
     ws, size, _kept = _workspace(lib.tg_rms_norm_grad_workspace_bytes(a), workspace, dy, device)
     T._check(lib.tg_rms_norm_grad(a, ws, size, _stream(device)), "tg_rms_norm_grad")
