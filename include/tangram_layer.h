@@ -23,10 +23,12 @@
  *   - Calls are asynchronous on `stream`, never synchronise and allocate
  *     nothing (tg_adamw_create excepted), so they can be captured in a graph.
  *     A workspace is 256-byte aligned and belongs to one call at a time.
- *   - Arithmetic is in 32 bits whatever the elements' type: products of
- *     16-bit and 8-bit elements accumulate in 32 bits, norms, statistics and
- *     moments are computed in 32 bits, and results are rounded once, to
- *     nearest even.  Results are repeatable bit for bit on one device.
+ *   - Arithmetic is in 32 bits whatever the elements' type: products
+ *     accumulate in 32 bits, norms, statistics and moments are computed in 32
+ *     bits, and results are rounded once, to nearest even.  (Products of 8-bit
+ *     elements in large sizes are added in groups of eight by the matrix
+ *     instruction, which drops what lies 2^-16 below a group's largest.)
+ *     Results are repeatable bit for bit on one device.
  *   - NaN and infinities propagate as the formulas say.
  *   - Errors: TG_EINVAL for an invalid argument, TG_ENOMEM for a workspace
  *     that is too small, TG_EDEVICE for a failed launch; tg_last_error() has
