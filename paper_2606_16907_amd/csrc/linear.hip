@@ -572,13 +572,14 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
 // rows may start anywhere; rows past an operand's end repeat its last, and what comes
 // of them is dropped.  8-bit operands become bf16, which is exact and costs
 // nothing that shows.
+constexpr int kFewWaves = 8, kTurnBytes = 512;
 template <typename T, typename O, int kRows>
-__global__ __launch_bounds__(512) void product_few(Product a, Epilogue e) {
+__global__ __launch_bounds__(512) void product_few(Product a, Epilogue e, int64_t share_turns) {
     using C = std::conditional_t<sizeof(T) == 1, bf16, T>;
     using frag = typename Matrix<C>::frag;
     using raw = typename Unit<T>::raw;
-    constexpr int kWaves = 8, kUnits = sizeof(T) == 1 ? 16 : 8;  // of 8 elements, of a lane in a turn
-    constexpr int kTurn = kUnits * 4 * 8;                       // elements of r in a turn
+    constexpr int kWaves = kFewWaves, kUnits = kTurnBytes / sizeof(T) / 32;  // of 8 elements, of a lane in a turn
+    constexpr int kTurn = kTurnBytes / sizeof(T);                            // elements of r in a turn
     __shared__ f32x4 sums[kWaves][kRows][64];
     const int wave = wave_index(), lane = threadIdx.x % 64;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
@@ -597,8 +598,9 @@ __global__ __launch_bounds__(512) void product_few(Product a, Epilogue e) {
             for (int m = 0; m < kRows; ++m) acc[m] = Matrix<C>::mma(fw, __builtin_bit_cast(frag, widened(ux[m][u])), acc[m]);
         }
     };
-    const int64_t whole = a.nr / kTurn;
-    for (int64_t turn = wave; turn < whole; turn += kWaves) {
+    // this block's share of the turns, whole ones but for the last of all
+    const int64_t begin = blockIdx.y * share_turns, whole = a.nr / kTurn, end = std::min(whole, begin + share_turns);
+    for (int64_t turn = begin + wave; turn < end; turn += kWaves) {
         raw uw[kUnits], ux[kRows][kUnits];
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) uw[u] = Unit<T>::load(w + turn * kTurn + at(u), 8);
@@ -608,7 +610,7 @@ __global__ __launch_bounds__(512) void product_few(Product a, Epilogue e) {
             for (int u = 0; u < kUnits; ++u) ux[m][u] = Unit<T>::load(x[m] + turn * kTurn + at(u), 8);
         multiply(uw, ux);
     }
-    if (whole * kTurn < a.nr && wave == whole % kWaves) {
+    if (whole * kTurn < a.nr && blockIdx.y + 1 == gridDim.y && wave == (whole - begin) % kWaves) {
         raw uw[kUnits], ux[kRows][kUnits];
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
@@ -628,7 +630,12 @@ __global__ __launch_bounds__(512) void product_few(Product a, Epilogue e) {
 #pragma unroll
         for (int h = 1; h < kWaves; ++h) z += sums[h][u / 64][u % 64];
         const int64_t i = u / 64 * 16 + u % 16, j = n0 + u % 64 / 16 * 4;
-        if (i < a.ni && j < a.nj) finish<O, 4>(z, i, j, (int)std::min<int64_t>(4, a.nj - j), e);
+        if (i >= a.ni || j >= a.nj) continue;
+        const int valid = (int)std::min<int64_t>(4, a.nj - j);
+        if (e.partial)
+            store_f32<float, 4>(e.partial + (blockIdx.y * a.ni + i) * a.nj + j, z, valid);
+        else
+            finish<O, 4>(z, i, j, valid, e);
     }
 }
 
@@ -733,13 +740,35 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
     // bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at 16.
     // Where an operand would have to be packed, up to 64 rows.
     p.few = !down_p && !down_q && a.ni <= (p.pack_p || p.pack_q ? 64 : 8);
-    if (p.few) return p;
+    if (p.few) {
+        // Few rows of w leave most of the chip idle: sums of 40 turns and more are
+        // shared out among blocks then, a turn a wave at least.  4 rows through 689 x
+        // 10803, whose rows are not aligned, take 23.5 us in one share and 12.8 in
+        // five, one through 1024 x 14336 18.6 and 13.2; through 1024 x 8192 11.5 and
+        // 13.4, which is another launch.
+        const int64_t blocks = ceil_div(a.nj, 16), turns = a.nr * size / kTurnBytes;
+        const int64_t most = blocks < 128 && turns >= 40 ? std::min<int64_t>(8, ceil_div(256, blocks)) : 1;
+        p.cut.splits = (int)std::max<int64_t>(1, std::min(most, turns / kFewWaves));
+        p.cut.share = (int)ceil_div(std::max<int64_t>(1, turns), p.cut.splits);
+        p.cut.splits = (int)std::max<int64_t>(1, ceil_div(turns, p.cut.share));
+        p.bytes = cut_bytes(p.cut, a.ni, a.nj);
+        return p;
+    }
     p.cut = cut_product(a.ni, a.nj, a.nr, size);
     const auto packed = [&](int64_t n, bool down) { return round256(down ? a.nr * whole_ld(n, size) * size : n * whole_ld(a.nr, size) * size); };
     p.p_bytes = p.pack_p ? packed(a.ni, down_p) : 0;
     p.q_bytes = p.pack_q ? packed(a.nj, down_q) : 0;
     p.bytes = p.p_bytes + p.q_bytes + cut_bytes(p.cut, a.ni, a.nj);
     return p;
+}
+
+// After a product's launch: its error, or the launch that adds up its shares.
+template <typename O>
+hipError_t join(const Product &a, const Epilogue &e, int splits, hipStream_t s) {
+    const hipError_t r = hipGetLastError();
+    if (r != hipSuccess || !e.partial) return r;
+    hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)ceil_div(a.ni * ceil_div(a.nj, 8), 256)), dim3(256), 0, s, e, splits, a.ni, a.nj);
+    return hipGetLastError();
 }
 
 // C; `ws` holds the plan's bytes.
@@ -750,14 +779,15 @@ hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hi
     const Plan p = plan_product(a, kSize, r_bytes_p, kDownP, kDownQ);
     if constexpr (!kDownP && !kDownQ) {
         if (p.few) {
-            const dim3 grid((unsigned)ceil_div(a.nj, 16));
+            const dim3 grid((unsigned)ceil_div(a.nj, 16), p.cut.splits);
+            e.partial = p.cut.splits > 1 ? (float *)ws : nullptr;
             switch ((a.ni + 15) / 16) {
-                case 1: hipLaunchKernelGGL((product_few<T, O, 1>), grid, dim3(512), 0, s, a, e); break;
-                case 2: hipLaunchKernelGGL((product_few<T, O, 2>), grid, dim3(512), 0, s, a, e); break;
-                case 3: hipLaunchKernelGGL((product_few<T, O, 3>), grid, dim3(512), 0, s, a, e); break;
-                default: hipLaunchKernelGGL((product_few<T, O, 4>), grid, dim3(512), 0, s, a, e);
+                case 1: hipLaunchKernelGGL((product_few<T, O, 1>), grid, dim3(512), 0, s, a, e, p.cut.share); break;
+                case 2: hipLaunchKernelGGL((product_few<T, O, 2>), grid, dim3(512), 0, s, a, e, p.cut.share); break;
+                case 3: hipLaunchKernelGGL((product_few<T, O, 3>), grid, dim3(512), 0, s, a, e, p.cut.share); break;
+                default: hipLaunchKernelGGL((product_few<T, O, 4>), grid, dim3(512), 0, s, a, e, p.cut.share);
             }
-            return hipGetLastError();
+            return join<O>(a, e, p.cut.splits, s);
         }
     }
     if ((p.pack_p || p.pack_q) && a.nr > 0) {
@@ -785,12 +815,7 @@ hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hi
         hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
     else
         hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
-    if (e.partial) {
-        const hipError_t r = hipGetLastError();
-        if (r != hipSuccess) return r;
-        hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)ceil_div(a.ni * ceil_div(a.nj, 8), 256)), dim3(256), 0, s, e, c.splits, a.ni, a.nj);
-    }
-    return hipGetLastError();
+    return join<O>(a, e, c.splits, s);
 }
 
 // ---------------------------------------------------------------------------

@@ -58,6 +58,22 @@ def test_forward_in_8_bits(m, k, n, out):
     R.within(plain, want, R.linear_bound(want, z, bound, BF16))
 
 
+@pytest.mark.parametrize("m,k,n,pad", [(1, 10240, 16, 0), (4, 10803, 689, 3), (5, 20483, 33, 5), (8, 14336, 1024, 0), (40, 10247, 100, 1)])
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_few_rows_with_long_sums(m, k, n, pad, dtype):
+    gen = R.generator("long", m, k, n, pad)
+    bias, residual = R.rows(gen, 1, n, BF16)[0], R.rows(gen, m, n, BF16, pad)
+    if dtype == E4M3:
+        k *= 2
+        x, sx = quantised(R.rows(gen, m, k, torch.float32))
+        w, sw = quantised(R.rows(gen, n, k, torch.float32, std=k ** -0.5))
+    else:
+        x, w, sx, sw = R.rows(gen, m, k, BF16, pad), R.rows(gen, n, k, BF16, pad, k ** -0.5), None, None
+    y = layer().tg_linear(x, w, bias=bias, act="silu", residual=residual, x_scale=sx, w_scale=sw)
+    want, z, bound = R.linear(x, w, bias, "silu", residual, sx, sw)
+    R.within(y, want, R.linear_bound(want, z, bound, BF16, residual))
+
+
 GRAD_SIZES = [(1, 1, 1), (1, 40, 24), (2, 17, 129), (16, 64, 64), (37, 100, 72), (64, 128, 256), (100, 1, 33), (129, 257, 65),
               (256, 256, 256), (300, 264, 520), (513, 72, 300), (1030, 130, 70)]
 
