@@ -61,10 +61,19 @@ struct Epilogue {
 __device__ inline float exp_f32(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // The normal distribution function from exp(-z^2 / 2), which its caller may need
-// too: erfc by formula 7.1.26 of Abramowitz and Stegun, off by at most 1.5e-7.
+// too.  Below 0 it is bell erfcx(|z| / sqrt 2) / 2, and that quotient is t P(t) with
+// t = 1 / (1 + 0.265 |z|): P of degree 6 was fitted to it by least squares, weighted
+// until its largest relative error up to |z| = 14.5 was least.  In 32 bits it is off by 1e-6
+// of its value, so gelu keeps its relative accuracy where it is small.
 __device__ inline float normal_cdf(float z, float bell) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-    const float tail = 0.5f * bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.265f, fabsf(z), 1.0f));
+    float p = fmaf(t, -0.067787044f, 0.19527312f);
+    p = fmaf(t, p, -0.06636293f);
+    p = fmaf(t, p, 0.14249334f);
+    p = fmaf(t, p, 0.08294658f);
+    p = fmaf(t, p, 0.10783678f);
+    p = fmaf(t, p, 0.105599836f);
+    const float tail = bell * t * p;
     return z >= 0.0f ? 1.0f - tail : tail;
 }
 
