@@ -84,7 +84,9 @@ tg_status tg_linear(const tg_linear_args *a, void *d_ws, size_t ws_bytes, tg_str
 /*
  * Gradients of tg_linear for 16-bit types, from dy [m, n]:
  *   dz = dy act'(z) with z from `pre` (which may be NULL for TG_ACT_NONE),
- *        rounded once to `type`, the type that the matrix instructions read;
+ *        rounded once to `type`, the type that the matrix instructions read
+ *        (where `pre` is an infinity, as a z beyond `type` is, act' has its
+ *        limit there, 0 or 1);
  *   dx [m, k] = dz w, dw [n, k] = dz^T x, dbias [n] = the sum of dz's rows
  *        (before dz is rounded).
  * dx, dw and dbias may be NULL where they are not wanted; they have the

@@ -91,8 +91,15 @@ __device__ inline void activate(vec<float, N> &z, int act) {
         for (int c = 0; c < N; ++c) z[c] *= normal_cdf(z[c], exp_f32(-0.5f * z[c] * z[c]));
     }
 }
+// z comes in 16 bits, where one that was finite may be an infinity.  At |z| = 128
+// the slopes of silu and gelu are 0 and 1 in 32 bits, so z is held there; NaN stays.
+__device__ inline float held(float z) { return fabsf(z) > 128.0f ? copysignf(128.0f, z) : z; }
 template <int N>
 __device__ inline vec<float, N> slope(vec<float, N> z, int act) {
+    if (act == TG_ACT_SILU || act == TG_ACT_GELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) z[c] = held(z[c]);
+    }
     if (act == TG_ACT_RELU) {
 #pragma unroll
         for (int c = 0; c < N; ++c) z[c] = z[c] > 0.0f ? 1.0f : 0.0f;
