@@ -111,7 +111,7 @@ tg_status tg_linear_grad(const tg_linear_grad_args *a, void *d_ws, size_t ws_byt
  *   hidden    [rows, cols] or NULL: receives h rounded to `type`, the residual
  *             stream of the next operator (it may be x or residual itself)
  *   y         for TG_E4M3: y / scale of the row, scale = max |y| / 448 over
- *             the row's finite values, 1 where that is 0
+ *             the row's finite values, 2^-126 at least, and 1 where those are 0
  *   scale     [rows] floats, TG_E4M3 only; rstd [rows] floats or NULL
  */
 typedef struct {

@@ -20,6 +20,8 @@ namespace {
 template <typename E>
 constexpr int kUnitOf = 16 / sizeof(E);
 
+constexpr float kLeastScale = 0x1p-126f;  // of an 8-bit output: the least normal number
+
 struct NormArgs {
     const void *x, *residual, *weight;
     void *hidden, *y;
@@ -133,8 +135,8 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
             }
         }
         most = block_reduce<OpMax, T>(most, slots[1]);
-        scale = most / kE4M3Max;
-        scale = scale > 0.0f ? scale : 1.0f;
+        // a subnormal scale has few bits, and a row's largest over it could pass 448
+        scale = most > 0.0f ? fmaxf(most / kE4M3Max, kLeastScale) : 1.0f;
         if (t == 0) a.scale[row] = scale;
     }
     if (kStream) {

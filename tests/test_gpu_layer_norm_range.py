@@ -1,0 +1,39 @@
+"""The norm at the ends of its range: rows of subnormal numbers, very many columns, outputs in the place of inputs."""
+import pytest
+import torch
+
+from tests import layer_ref as R
+from tests.layer_ref import E4M3, E32, U
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def layer():
+    from paper_2606_16907_amd import layer as L
+    return L
+
+
+@pytest.mark.parametrize("cols", [40, 3000, 33000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_8_bits_of_rows_whose_scale_would_be_subnormal(cols, dtype):
+    """|y| from 2^-149 to 2^-100: the scale is no less than 2^-126, so no code passes 448, and scale times code is within
+    half a step of the code (2^-4 of it, 2^-10 of the scale below 2^-6) of y."""
+    gen = R.generator("subnormal", cols, dtype)
+    # first, a row whose largest is 668 of the smallest numbers: over a scale of one of them no code holds it
+    exponents = (-149, -146, -142, -141, -140, -139, -133, -130, -126, -120, -118, -117, -110, -100)
+    small = [382 * 2.0 ** -149] + [2.0 ** e for e in exponents]
+    # rows of +-1 have rstd = 1 - 5e-7 and y = +-weight; the weight's largest element sets the row's scale
+    for top in small:
+        x = torch.where(torch.rand(2, cols, generator=gen) < 0.5, -1.0, 1.0).to(dtype).cuda()
+        w = (torch.rand(cols, generator=gen, dtype=torch.float64) * top).to(dtype)
+        w[0] = top * 1.75
+        w = w.cuda()
+        f = layer().tg_rms_norm(x, w, out_dtype=E4M3)
+        y = R.f64(x) * R.f64(w) * (1 + 1e-6) ** -0.5
+        got, scale = R.f64(f.y.float()), R.f64(f.scale)[:, None]
+        assert bool(torch.isfinite(got).all()), top
+        # the kernel's own y is a subnormal of 2^-149 where it is one at all
+        bound = (2.0 ** -4 * 1.001) * y.abs() + 2.0 ** -10 * 1.001 * scale + 2.0 ** -149 + (cols / 64 + 40) * E32 * y.abs()
+        R.within(got * scale, y, bound, f"top {top}")
+        assert bool((scale >= 2.0 ** -126).all()), top
