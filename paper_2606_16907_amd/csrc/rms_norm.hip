@@ -163,7 +163,7 @@ struct GradArgs {
     void *dx;
     float *partial;  // [gridDim.x, cols] sums of dy h rstd
     int64_t rows, lddy, lddh, ldh, lddx;
-    int64_t first;  // row of block 0 (norm_grad_stream)
+    int64_t first;  // of block 0: its unit of columns (norm_grad_weight_stream), its row (norm_grad_stream)
     int cols;
     float inv_cols;
 };
@@ -245,9 +245,9 @@ template <typename E>
 __global__ __launch_bounds__(256) void norm_grad_weight_stream(GradArgs a) {
     constexpr int kUnit = kUnitOf<E>;
     using unit = vec<float, kUnit>;
-    const int u = blockIdx.y * 256 + threadIdx.x;
-    if (u * (int64_t)kUnit >= a.cols) return;
-    const int col = u * kUnit, valid = left_of(a.cols, col);
+    const int64_t u = a.first + (int64_t)blockIdx.y * 256 + threadIdx.x;
+    if (u * kUnit >= a.cols) return;
+    const int col = (int)u * kUnit, valid = left_of(a.cols, col);
     unit dw(0.0f);
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const unit g = load_f32<E, kUnit>((const E *)a.dy + row * a.lddy + col, valid);
@@ -350,8 +350,12 @@ hipError_t launch_grad(GradArgs a, hipStream_t s) {
     } else if (units <= kMost) {
         go(norm_grad_kernel<E, 1024, kMost / 1024>, 1024);
     } else {
-        hipLaunchKernelGGL(norm_grad_weight_stream<E>, dim3(grid.x, (unsigned)ceil_div(units, 256)), dim3(256), 0, s, a);
-        for (; a.first < a.rows; a.first += kMostBlocks)
+        constexpr int64_t kMostUnits = 1 << 20;  // of a launch: 2^12 blocks across the columns by 512 down the rows
+        for (; a.first < units; a.first += kMostUnits) {
+            const dim3 blocks(grid.x, (unsigned)ceil_div(std::min(kMostUnits, units - a.first), 256));
+            hipLaunchKernelGGL(norm_grad_weight_stream<E>, blocks, dim3(256), 0, s, a);
+        }
+        for (a.first = 0; a.first < a.rows; a.first += kMostBlocks)
             hipLaunchKernelGGL(norm_grad_stream<E>, dim3((unsigned)std::min(kMostBlocks, a.rows - a.first)), dim3(1024), 0, s, a);
     }
     return hipGetLastError();

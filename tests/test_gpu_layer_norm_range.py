@@ -37,3 +37,26 @@ def test_8_bits_of_rows_whose_scale_would_be_subnormal(cols, dtype):
         bound = (2.0 ** -4 * 1.001) * y.abs() + 2.0 ** -10 * 1.001 * scale + 2.0 ** -149 + (cols / 64 + 40) * E32 * y.abs()
         R.within(got * scale, y, bound, f"top {top}")
         assert bool((scale >= 2.0 ** -126).all()), top
+
+
+def test_the_gradient_of_half_a_billion_columns():
+    """A pattern of 1033 columns, over and over: sums over a row are the pattern's, the weight's gradient repeats too."""
+    period, times = 1033, 519721
+    cols = period * times
+    assert cols > 1 << 29
+    gen = R.generator("wide")
+    dy, h, w = (R.rows(gen, m, period, BF16) for m in (2, 2, 1))
+    rstd = torch.tensor([0.75, 1.25], device="cuda")
+    dx, dw = layer().tg_rms_norm_grad(dy.repeat(1, times), h.repeat(1, times), w[0].repeat(times), rstd)
+    s = R.f64(rstd)[:, None]
+    g, xhat = R.f64(dy) * R.f64(w), R.f64(h) * s
+    mean, size = (g * xhat).mean(1, keepdim=True), (g * xhat).abs().mean(1, keepdim=True)
+    want = s * (g - xhat * mean)
+    # 1024 threads add up a row, cols / 1024 products each, one rounding an addition and one a product
+    bound = s * (xhat.abs() * ((cols / 1024 + 32) * E32 * size + 8 * E32 * mean.abs()) + 8 * E32 * g.abs()) + (8 * E32 + 1.01 * U[BF16]) * want.abs()
+    term = R.f64(dy) * xhat
+    for got, want, bound in ((dx, want, bound), (dw[None], term.sum(0)[None], (1.01 * U[BF16] * term.sum(0).abs() + 18 * E32 * term.abs().sum(0))[None])):
+        for row in range(got.shape[0]):
+            far = (got[row].view(times, period).float() - want[row].float().cuda()).abs_()
+            # the oracle was rounded to 32 bits for this
+            assert bool((far <= (bound[row] + 2 * E32 * want[row].abs()).float().cuda()).all()), row
