@@ -313,7 +313,7 @@ class AdamW:
         lib = load_library()
         ts = self.tensors
         params = ts["param"]
-        self.device = torch.cuda.current_device()
+        device = torch.cuda.current_device()
         dtype = params[0].dtype if params else torch.float32
         grad = ts["grad"][0].dtype if ts["grad"] else dtype
         state = ts["m"][0].dtype if ts["m"] else torch.float32
@@ -336,8 +336,8 @@ class AdamW:
                 n = params[i].numel()
                 if name.endswith("scale"):
                     n = -(-n // SCALE_BLOCK)
-                if t.get_device() != self.device:
-                    raise _elsewhere(t, f"{name} {i}", self.device)
+                if t.get_device() != device:
+                    raise _elsewhere(t, f"{name} {i}", device)
                 if t.dtype != want[name]:
                     raise ValueError(f"{name} {i}: dtype {t.dtype}, {want[name]} expected")
                 if not t.is_contiguous() or t.numel() != n:
@@ -349,7 +349,7 @@ class AdamW:
         T._check(lib.tg_adamw_create(table, len(params), TYPES[dtype], TYPES[grad], 8 if eight else 32,
                                      ctypes.byref(h)), "tg_adamw_create")
         self.close()
-        self.h = h
+        self.h, self.device = h, device
 
     def set_grads(self, grads):
         """Takes other gradient buffers; waits for the device."""
