@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "sizes.h"
 #include "tangram_layer.h"
 
 namespace tg {
@@ -140,8 +141,5 @@ __device__ inline float block_reduce(float x, float *slots) {
 // out[c] = the sum of partial[r][c] over rows r (reduce.hip: ascending r within
 // eight interleaved strands, then the strands in order).
 hipError_t launch_column_sums(const float *partial, int rows, int64_t cols, void *out, int type, hipStream_t s);
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace tg
