@@ -53,10 +53,55 @@ def test_the_gradient_of_half_a_billion_columns():
     mean, size = (g * xhat).mean(1, keepdim=True), (g * xhat).abs().mean(1, keepdim=True)
     want = s * (g - xhat * mean)
     # 1024 threads add up a row, cols / 1024 products each, one rounding an addition and one a product
-    bound = s * (xhat.abs() * ((cols / 1024 + 32) * E32 * size + 8 * E32 * mean.abs()) + 8 * E32 * g.abs()) + (8 * E32 + 1.01 * U[BF16]) * want.abs()
+    bound = s * (xhat.abs() * ((cols / 1024 + 32) * E32 * size + 8 * E32 * mean.abs()) + 8 * E32 * g.abs())
+    bound = bound + (8 * E32 + 1.01 * U[BF16]) * want.abs()
     term = R.f64(dy) * xhat
-    for got, want, bound in ((dx, want, bound), (dw[None], term.sum(0)[None], (1.01 * U[BF16] * term.sum(0).abs() + 18 * E32 * term.abs().sum(0))[None])):
+    dw_bound = 1.01 * U[BF16] * term.sum(0).abs() + 18 * E32 * term.abs().sum(0)
+    for got, want, bound in ((dx, want, bound), (dw[None], term.sum(0)[None], dw_bound[None])):
         for row in range(got.shape[0]):
             far = (got[row].view(times, period).float() - want[row].float().cuda()).abs_()
             # the oracle was rounded to 32 bits for this
             assert bool((far <= (bound[row] + 2 * E32 * want[row].abs()).float().cuda()).all()), row
+
+
+WIDTHS = [1, 999, 1000, 16390, 33000]  # kept in registers, and read again for each pass
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_dx_in_the_place_of_dy_or_dhidden(cols, dtype):
+    L = layer()
+    gen = R.generator("alias", cols, dtype)
+    rows = 700 if cols < 2000 else 3
+    dy, hidden, dh = (R.rows(gen, rows, cols, dtype, 3) for _ in range(3))
+    w, rstd = R.rows(gen, 1, cols, dtype)[0], 0.5 + torch.rand(rows, generator=gen).cuda()
+    dx, dw = L.tg_rms_norm_grad(dy, hidden, w, rstd, dhidden=dh)
+    for which in (0, 1):
+        buffers = [dy.clone(), dh.clone()]
+        got, dweight = L.tg_rms_norm_grad(buffers[0], hidden, w, rstd, dhidden=buffers[1], dx=buffers[which])
+        assert got is buffers[which] and torch.equal(got, dx) and torch.equal(dweight, dw)
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_hidden_in_the_place_of_x_or_residual(cols, dtype, eight):
+    """The C call's form; the binding allocates hidden."""
+    from paper_2606_16907_amd import tangram as T
+    L = layer()
+    gen = R.generator("hidden", cols, dtype)
+    rows = 700 if cols < 2000 else 3
+    x, r = R.rows(gen, rows, cols, dtype), R.rows(gen, rows, cols, dtype)
+    w = R.rows(gen, 1, cols, dtype)[0]
+    want = L.tg_rms_norm(x, w, residual=r, out_dtype=E4M3 if eight else dtype, keep_rstd=True)
+    for which in (0, 1):
+        b = [x.clone(), r.clone()]
+        y, rstd = torch.empty_like(want.y), torch.empty_like(want.rstd)
+        scale = torch.empty_like(want.scale) if eight else None
+        a = L.TgRmsNormArgs(x=b[0].data_ptr(), residual=b[1].data_ptr(), weight=w.data_ptr(), hidden=b[which].data_ptr(), y=y.data_ptr(),
+                            scale=scale.data_ptr() if eight else None, rstd=rstd.data_ptr(), rows=rows, cols=cols, ldx=cols, ldr=cols,
+                            ldh=cols, ldy=cols, eps=1e-6, type=L.TYPES[dtype], out_type=L.TYPES[y.dtype])
+        T._check(L.load_library().tg_rms_norm(a, torch.cuda.current_stream().cuda_stream), "tg_rms_norm")
+        assert torch.equal(b[which], want.hidden) and torch.equal(y.view(torch.uint8), want.y.view(torch.uint8))
+        assert torch.equal(rstd, want.rstd) and (not eight or torch.equal(scale, want.scale))
+        assert torch.equal(b[1 - which], (x, r)[1 - which])
