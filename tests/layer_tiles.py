@@ -1,8 +1,9 @@
-"""Sizes whose products go through tiles of 256 x 256, one pass of tiles over the GPU and more than one turn of the loop
-over r among them.  (m, k, n, pad, type): pad is the columns by which the operands' rows are wider, 3 where they do not
+"""Sizes whose products go through tiles of 256 x 256, in one pass over the GPU but for the last of FORWARD, with few and
+with many steps of r.  (m, k, n, pad, type): pad is the columns by which the operands' rows are wider, 3 where they do not
 start at 16-byte addresses, 5 where odd rows do."""
 FORWARD = [(3500, 1000, 4075, 8, "bf16"), (3841, 72, 3841, 0, "fp16"), (3500, 1003, 4075, 3, "fp16"),
-           (3300, 136, 3400, 8, "bf16"), (1500, 8200, 3000, 0, "bf16"), (1500, 8199, 3001, 3, "fp16")]
+           (3300, 136, 3400, 8, "bf16"), (1500, 8200, 3000, 0, "bf16"), (1500, 8199, 3001, 3, "fp16"),
+           (8200, 1000, 8100, 8, "bf16")]
 EIGHT = [(3500, 2064, 4075, 16, "e4m3"), (3841, 1999, 3841, 3, "e4m3"), (3300, 144, 3400, 0, "e4m3"),
          (3000, 16400, 1500, 0, "e4m3")]
 # dx [m, k] = dz w with sums over n, dw [n, k] = dz^T x with sums over m
