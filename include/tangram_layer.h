@@ -62,7 +62,8 @@ typedef enum { TG_ACT_NONE = 0, TG_ACT_RELU = 1, TG_ACT_SILU = 2, TG_ACT_GELU = 
  *   bias      [n] or NULL; residual [m, n] or NULL
  *   pre       [m, n] or NULL: receives z, which tg_linear_grad takes
  * residual may be y itself (added in place).  m < 2^31 - 256, n and k at most
- * 2^21 - 64.
+ * 2^21 - 64, and fewer than 2^24 tiles of 128 x 128 in each of [m, n], [m, k]
+ * and [n, k].
  */
 typedef struct {
     const void *x, *w;

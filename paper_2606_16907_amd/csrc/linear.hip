@@ -876,9 +876,8 @@ tg_status check_workspace(const void *ws, size_t bytes, size_t need) {
 bool sizes_fit(int64_t m, int64_t n, int64_t k) {
     const int64_t most = kMostLd - 64;
     return m >= 0 && n >= 0 && k >= 0 && m <= 0x7fffffff - 256 && n <= most && k <= most &&
-           // a grid holds fewer than 2^32 threads
-           ceil_div(m, 128) * ceil_div(std::max(n, k), 128) < (1 << 24) && ceil_div(n, 128) * ceil_div(k, 128) < (1 << 24) &&
-           m * ceil_div(std::max(n, k), 8) < (int64_t)1 << 32;
+           // a grid holds fewer than 2^32 threads, 256 a tile of 128 x 128 (shares are joined for 2^26 elements at most)
+           ceil_div(m, 128) * ceil_div(std::max(n, k), 128) < (1 << 24) && ceil_div(n, 128) * ceil_div(k, 128) < (1 << 24);
 }
 
 // A row stride that may be used where there are fewer than two rows, too.
