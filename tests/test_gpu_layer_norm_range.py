@@ -105,3 +105,27 @@ def test_hidden_in_the_place_of_x_or_residual(cols, dtype, eight):
         assert torch.equal(b[which], want.hidden) and torch.equal(y.view(torch.uint8), want.y.view(torch.uint8))
         assert torch.equal(rstd, want.rstd) and (not eight or torch.equal(scale, want.scale))
         assert torch.equal(b[1 - which], (x, r)[1 - which])
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 22) + 5, 8), ((1 << 20) + 3, 1025)])
+def test_more_rows_than_a_launch_takes(rows, cols):
+    """Rows repeat, so every row of the result is that of the first ones, and the weight's gradient adds up all of them."""
+    L, period = layer(), 16
+    gen = R.generator("many rows", rows, cols)
+    x, r, dy = (R.rows(gen, period, cols, BF16) for _ in range(3))
+    w = R.rows(gen, 1, cols, BF16)[0]
+    which = torch.arange(rows, device="cuda") % period
+    few, many = L.tg_rms_norm(x, w, residual=r), L.tg_rms_norm(x[which], w, residual=r[which])
+    for a, b in ((few.y, many.y), (few.hidden, many.hidden), (few.rstd, many.rstd)):
+        assert torch.equal(a[which], b)
+    eight = L.tg_rms_norm(x, w, residual=r, out_dtype=E4M3), L.tg_rms_norm(x[which], w, residual=r[which], out_dtype=E4M3)
+    assert torch.equal(eight[0].y.view(torch.uint8)[which], eight[1].y.view(torch.uint8))
+    assert torch.equal(eight[0].scale[which], eight[1].scale)
+    dx, _ = L.tg_rms_norm_grad(dy, few.hidden, w, few.rstd)
+    got, dw = L.tg_rms_norm_grad(dy[which], many.hidden, w, many.rstd)
+    assert torch.equal(dx[which], got)
+    times = torch.bincount(which).double().cpu()[:, None]
+    term = times * R.f64(dy) * R.f64(few.hidden) * R.f64(few.rstd)[:, None]
+    # 512 blocks add up rows / 512 products each, then 64 of their sums in a strand and 8 strands
+    bound = 1.01 * U[BF16] * term.sum(0).abs() + (rows / 512 + 96) * E32 * term.abs().sum(0)
+    R.within(dw, term.sum(0), bound, "dweight")
