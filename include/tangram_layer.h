@@ -27,7 +27,8 @@
  *     accumulate in 32 bits, norms, statistics and moments are computed in 32
  *     bits, and results are rounded once, to nearest even.  (Products of 8-bit
  *     elements in large sizes are added in groups of eight by the matrix
- *     instruction, which drops what lies 2^-16 below a group's largest.)
+ *     instruction, which drops what lies 2^-16 below a group's largest;
+ *     those of a few rows of x are exact.)
  *     Results are repeatable bit for bit on one device.
  *   - NaN and infinities propagate as the formulas say.
  *   - Errors: TG_EINVAL for an invalid argument, TG_ENOMEM for a workspace
@@ -110,10 +111,13 @@ tg_status tg_linear_grad(const tg_linear_grad_args *a, void *d_ws, size_t ws_byt
  *   type      of x, residual, weight and hidden: TG_F32, TG_BF16 or TG_F16
  *   out_type  of y: `type` or TG_E4M3
  *   hidden    [rows, cols] or NULL: receives h rounded to `type`, the residual
- *             stream of the next operator (it may be x or residual itself)
+ *             stream of the next operator (it may be x or residual itself);
+ *             y is computed from h before that rounding
  *   y         for TG_E4M3: y / scale of the row, scale = max |y| / 448 over
  *             the row's finite values, 2^-126 at least, and 1 where those are 0
  *   scale     [rows] floats, TG_E4M3 only; rstd [rows] floats or NULL
+ * rows < 2^31, cols < 2^31 - 64.  Squares are added in 32 bits: rows with |h|
+ * beyond 1.8e19 have rstd 0.
  */
 typedef struct {
     const void *x, *residual, *weight;
@@ -132,7 +136,8 @@ tg_status tg_rms_norm(const tg_rms_norm_args *a, tg_stream stream);
  * dhidden (NULL: none): with g = dy weight
  *   dx = dhidden + rstd (g - h rstd^2 mean(g h)), the gradient of x and of the
  *        residual alike;  dweight[c] = the sum over rows of dy h rstd.
- * hidden and rstd are tg_rms_norm's.  dx may be dy or dhidden itself.
+ * hidden and rstd are tg_rms_norm's; h is read as hidden holds it, rounded.  dx
+ * may be dy or dhidden itself.
  */
 typedef struct {
     const void *dy, *dhidden, *hidden, *weight;
@@ -194,7 +199,8 @@ typedef struct tg_adamw tg_adamw;
 tg_status tg_adamw_create(const tg_adamw_tensor *tensors, int32_t n_tensors, int32_t param_type,
                           int32_t grad_type, int32_t state_bits, tg_adamw **out);
 /* One step over every tensor.  Steps of one handle must be ordered (one stream,
-   or events). */
+   or events).  A graph that captured a step reads the handle's table at every
+   replay: the handle must outlive it. */
 tg_status tg_adamw_step(const tg_adamw *a, const tg_adamw_rates *rates, tg_stream stream);
 /* Waits for the device and frees the table (NULL is ignored). */
 void tg_adamw_destroy(tg_adamw *a);

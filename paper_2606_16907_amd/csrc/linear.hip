@@ -200,11 +200,12 @@ __device__ inline i32x4 widened(vec<int, 2> u) {
 // multiplied, across steps too, so the matrix instructions wait at one barrier a
 // step, which stands between the halves: there every wave has read all of the
 // step's tiles, whose places later ones take, and the next have arrived.  Four
-// waves of 128 x 128 read each byte of LDS half as often as eight of 128 x 64
-// would.  8192^3 in bf16 takes 790 to 900 us (1220 to 1390 TFLOP/s; this card's
-// library products reach 1180 to 1580), in 8 bits 379 (2900); leaving out the loads
-// saves 12% of that, the reads 13%: what remains is the matrix instructions at the
-// 1.4 to 1.8 GHz that the power allows.
+// waves of 128 x 128 read a step's tiles twice, P and Q alike; eight of 128 x 64
+// would read P four times.  8192^3 in bf16 takes 780 to 880 us in every order of
+// the operands (1250 to 1420 TFLOP/s; this card's library products 680 to 800 for x w^T,
+// 780 to 900 for dz w and 920 to 1020 for dz^T x), in 8 bits 379 (2900); leaving out
+// the loads saves 12% of that, the reads 13%: what remains is the matrix
+// instructions at the 1.4 to 1.8 GHz that the power allows.
 template <typename T>
 struct Wide;  // 32 x 32 matrix instructions: kDeep of them over half a step's r
 template <>
@@ -582,8 +583,9 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
 // ---------------------------------------------------------------------------
 // Bound by reading w once.  A block has 16 rows of w and all rows of x, 16 kRows
 // of them; its eight waves take turns at r, 512 bytes of each row of w a turn, and
-// add up their sums through LDS: one row through 4096 x 14336 in bf16 takes 23.4
-// us, 5.0 TB/s (256 bytes a turn 25.2).  Operands go from memory to registers, so
+// add up their sums through LDS: one row through 4096 x 14336 in bf16 takes 23.5
+// us, 5.0 TB/s (256 bytes a turn 25.2; the library's product 27.3), in 8 bits 16.2,
+// and eight rows 17.9.  Operands go from memory to registers, so
 // rows may start anywhere; rows past an operand's end repeat its last, and what comes
 // of them is dropped.  8-bit operands become bf16, which is exact and costs
 // nothing that shows.
@@ -812,7 +814,10 @@ struct SlopeArgs {
 };
 
 // 256 columns by 8 rows at a time; a block goes down its share of the rows and
-// leaves one row of sums.  dz's rows are padded with zeros to ldz.
+// leaves one row of sums.  dz's rows are padded with zeros to ldz.  z is what the
+// forward pass kept of it in 16 bits, and dz is rounded to 16 bits because the
+// matrix instructions of the two products read no more; the bias's sums take it
+// before that.  Bound by memory: 8192 x 6144 in bf16 takes 59 us, 5.1 TB/s.
 template <typename E>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     using f32x8 = vec<float, 8>;

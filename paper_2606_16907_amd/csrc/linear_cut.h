@@ -16,9 +16,11 @@ constexpr int kStepBytes = 128;  // of r in a step of the loop over it
 // 1.05 while few of the 256 CUs work and 1.58 when all do, one of a 128 tile 0.38
 // to 0.56 alone on its CU and 0.95 beside another; beginning and end of a tile
 // take 9 and 3 to 5; the shares of a split are written and read at 4 TB/s, at 8
-// while the caches hold them, in a launch of 3.  2048 x 1024 x 4096: 24 in tiles of 128 and 36 of 256; 4096^3: 125
-// of 128 and 110 of 256; its gradient with sums of 4096 over 2048 x 1024: 34
-// unsplit, 29 in two.  Tiles of 256 x 128 were within 5% of the better of the two.
+// while the caches hold them, in a launch of 3.  2048 x 1024 x 4096: 24 in tiles
+// of 128 and 36 of 256; 4096^3: 125 of 128 and 110 of 256; its gradient with sums
+// of 4096 over 2048 x 1024: 34 unsplit, 29 in two.  Tiles of 256 x 128 were within
+// 5% of the better of the two.  The epilogue's operands are not counted: with them
+// and unaligned rows a short product takes up to twice the estimate, in either tile.
 struct Cut {
     int tile, splits, share;  // share: steps of a split
 };

@@ -6,9 +6,16 @@
 // stays in registers between its statistic and its output.  A row is cut into
 // units of 16 bytes; thread t of the row's T threads holds units t, t + T, ...
 // (N of them), every load of the row in flight before the reduction.  8192 x 8192
-// in bf16 takes 90 us forward (6.0 TB/s) and 118 backward (4.6 TB/s), where a large
-// copy reaches 4.8; forward with 256 threads a row took 96, backward with 768 or
-// 1024 blocks 24 and 11 more in all, with the next row fetched ahead the same.
+// in bf16 takes 89 us forward (6.0 TB/s), as much with 8 bits out, and 117
+// backward (4.6 TB/s), where a large copy reaches 4.8 to 4.9; forward with 256
+// threads a row took 96, backward with 768 or 1024 blocks 24 and 11 more in all,
+// with the next row fetched ahead the same.  The gradient of short rows is bound
+// by latency instead: its 512 blocks have a wave each up to 64 units a row, and
+// 16384 x 512 in bf16 takes 47 us, 1.4 TB/s.
+//
+// hidden is h rounded once to the inputs' type, which is what the next operator
+// and the gradient read; y is of the h before that rounding.  In 16 bits with a
+// residual the gradients so carry the error of one rounding beside their own.
 #include <algorithm>
 #include <cmath>
 
@@ -51,7 +58,7 @@ __device__ inline void store_e4m3(unsigned char *p, vec<float, kUnit> q, int val
     }
 }
 
-// One row per T threads, N units a thread (T N units or more), 256 / T rows a block
+// One row per T threads, N units a thread (T N units or fewer), 256 / T rows a block
 // where T is 64.  kStream: rows of any length, read again for each pass (x and
 // residual add up to the same h every time), one row a block.
 template <typename E, bool kEight, int T, int N, bool kStream>
@@ -303,9 +310,10 @@ hipError_t launch_norm(NormArgs a, hipStream_t s) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, a);
         }
     };
-    // A wave a row while a row is at most two units a lane; beyond that the
-    // fewest threads that hold a row in 4 units each.  Few rows leave most of
-    // the chip idle whatever is done, so they take more threads a row.
+    // A wave a row while a row is at most two units a lane; beyond that 256 to
+    // 1024 threads with one or two units each, and four only in rows of more than
+    // 2048 units.  Few rows leave most of the chip idle whatever is done, so
+    // they take more threads a row.
     if (units <= 64)
         go(norm_kernel<E, kEight, 64, 1, false>, 256, 4);
     else if (units <= 128)

@@ -13,7 +13,9 @@ Argument marshalling only, as in the submodule `tangram`: the work is done by
 the HIP kernels of libtangram_hip.so on torch's current stream, there is no CPU
 fallback, and every buffer is checked here for what a plain pointer cannot
 carry.  Matrices are two-dimensional tensors with unit stride along a row and
-any row stride.  Outputs are allocated unless they are given.
+any row stride.  Outputs are allocated unless they are given.  Nothing is
+recorded for autograd: a result never requires a gradient, whatever the inputs
+do, and gradients are calls of their own.
 """
 from __future__ import annotations
 
@@ -299,7 +301,9 @@ class AdamW:
 
     Tensors are contiguous and of any shape; their buffers are kept, so
     gradients are written in place from step to step (set_grads takes new
-    ones).  A step belongs to the stream that is current when it is called."""
+    ones).  A step belongs to the stream that is current when it is called.  A
+    graph that captured a step is not to be replayed after set_grads or close,
+    which free the table it reads."""
 
     def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, masters=None):
         self.tensors = dict(param=list(params), grad=list(grads), m=list(m), v=list(v))
@@ -352,7 +356,8 @@ class AdamW:
         self.h, self.device = h, device
 
     def set_grads(self, grads):
-        """Takes other gradient buffers; waits for the device."""
+        """Takes other gradient buffers; waits for the device.  Graphs that
+        captured a step before must be captured anew."""
         kept = self.tensors["grad"]
         self.tensors["grad"] = list(grads)
         try:

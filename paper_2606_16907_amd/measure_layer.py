@@ -11,6 +11,8 @@ of `layer`: norm and residual, up projection with bias and activation, down
 projection onto the residual stream, their gradients, and the AdamW step; and
 prints the efficiency eta that its products reach, the optimizer's time and bytes
 a parameter, and the plan of an instance with eta 1 and with the measured one.
+The plan takes eta alone, as a part of the peak of every island's GPUs; attention
+and gated projections are not among the operators and are taken to reach it too.
 """
 from __future__ import annotations
 
