@@ -7,8 +7,14 @@
  * master copy and two moments.  These are the operators behind those prices:
  *   tg_linear, tg_linear_grad       matrix product with bias, activation and
  *                                   residual in its epilogue, and its gradients
+ *   tg_gated, tg_gated_grad         gate and up projections, the activation and
+ *                                   their product, and their gradients
+ *   tg_block_linear                 matrix product of 8-bit operands with a scale
+ *                                   for every block of 128
+ *   tg_quantize                     its operands: 8-bit values and their scales
  *   tg_rms_norm, tg_rms_norm_grad   root-mean-square norm with the residual's
  *                                   addition, output in 16, 32 or 8 bits
+ *   tg_layer_norm, tg_layer_norm_grad   layer norm, the same way
  *   tg_adamw_*                      optimizer step over many tensors at once
  *
  * Conventions (those of tangram.h where not said otherwise):
@@ -27,7 +33,8 @@
  *     accumulate in 32 bits, norms, statistics and moments are computed in 32
  *     bits, and results are rounded once, to nearest even.  (Products of 8-bit
  *     elements in large sizes are added in groups of eight by the matrix
- *     instruction, which drops what lies 2^-16 below a group's largest;
+ *     instruction, which cuts each off at 2^-13 of the power of two in a
+ *     group's largest;
  *     those of a few rows of x are exact.)
  *     Results are repeatable bit for bit on one device.
  *   - NaN and infinities propagate as the formulas say.
@@ -45,8 +52,9 @@ extern "C" {
 #endif
 
 /* Element types.  TG_E4M3 is the 8-bit float with 4 exponent and 3 mantissa
-   bits, no infinities, largest value 448. */
-typedef enum { TG_F32 = 0, TG_BF16 = 1, TG_F16 = 2, TG_E4M3 = 3 } tg_dtype;
+   bits, no infinities, largest value 448.  TG_E8M0, of scales alone, is the power
+   of two 2^(code - 127), code 255 NaN. */
+typedef enum { TG_F32 = 0, TG_BF16 = 1, TG_F16 = 2, TG_E4M3 = 3, TG_E8M0 = 4 } tg_dtype;
 
 /* Activations: max(z, 0); z sigmoid(z); z Phi(z) with the normal distribution
    function Phi (no approximation by tanh). */
@@ -106,6 +114,98 @@ size_t tg_linear_grad_workspace_bytes(const tg_linear_grad_args *a);
 tg_status tg_linear_grad(const tg_linear_grad_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
 
 /*
+ * y = act(gate) up, gate = x w_gate^T + gate_bias, up = x w_up^T + up_bias, with x
+ * [m, k], w_gate and w_up [n, k], y [m, n].
+ *   type, out_type  as in tg_linear; biases, y, gate and up have out_type
+ *   x_scale   [m], gate_scale [n], up_scale [n] floats: with TG_E4M3 the products
+ *             are multiplied by them before the biases are added (all or none);
+ *             NULL otherwise
+ *   gate_bias, up_bias   [n] or NULL, each
+ *   gate, up  [m, n] or NULL, both or neither: receive gate and up, which
+ *             tg_gated_grad takes; y is computed before they are rounded
+ * The two weights may be halves of one matrix.  m < 2^31 - 256, n at most 2^20 -
+ * 64, k at most 2^21 - 64, and fewer than 2^24 tiles of 128 x 128 in each of
+ * [m, 2 n], [m, k] and [2 n, k].
+ */
+typedef struct {
+    const void *x, *w_gate, *w_up;
+    const float *x_scale, *gate_scale, *up_scale;
+    const void *gate_bias, *up_bias;
+    void *y, *gate, *up;
+    int64_t m, n, k;
+    int64_t ldx, ldwg, ldwu, ldy, ldg, ldu;
+    int32_t type, out_type, act, reserved; /* reserved must be 0 */
+} tg_gated_args;
+
+/* Bytes of workspace, as tg_linear_workspace_bytes. */
+size_t tg_gated_workspace_bytes(const tg_gated_args *a);
+tg_status tg_gated(const tg_gated_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
+
+/*
+ * Gradients of tg_gated for 16-bit types, from dy [m, n] and what it kept:
+ *   dgate = dy up act'(gate), dup = dy act(gate), each rounded once to `type`, the
+ *        type that the matrix instructions read (act' as in tg_linear_grad);
+ *   dx [m, k] = dgate w_gate + dup w_up, dw_gate [n, k] = dgate^T x, dw_up [n, k] =
+ *        dup^T x, dgate_bias and dup_bias [n] = the sums of dgate's and dup's rows
+ *        (before those are rounded).
+ * Each output may be NULL where it is not wanted.
+ */
+typedef struct {
+    const void *dy, *gate, *up, *x, *w_gate, *w_up;
+    void *dx, *dw_gate, *dw_up, *dgate_bias, *dup_bias;
+    int64_t m, n, k;
+    int64_t lddy, ldg, ldu, ldx, ldwg, ldwu, lddx, lddwg, lddwu;
+    int32_t type, act;
+} tg_gated_grad_args;
+
+size_t tg_gated_grad_workspace_bytes(const tg_gated_grad_args *a);
+tg_status tg_gated_grad(const tg_gated_grad_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
+
+/*
+ * y = act(z) + residual, z[i][j] = bias[j] + the sum over blocks b of 128 of k of
+ *     x_scale[i][b] w_scale[j / 128][b] (the sum over r in b of x[i][r] w[j][r]),
+ * with x [m, k] and w [n, k] of TG_E4M3, y [m, n].
+ *   x_scale   [m, ceil(k / 128)], w_scale [ceil(n / 128), ceil(k / 128)], both of
+ *             scale_type, TG_F32 or TG_E8M0; matrices with row strides ldxs, ldws
+ *   out_type  of bias, residual and y: TG_BF16 or TG_F16
+ *   bias      [n] or NULL; residual [m, n] or NULL, may be y itself
+ * A block's sum is added to the others in 32 bits after it is scaled.  Sizes as in
+ * tg_linear.
+ */
+typedef struct {
+    const void *x, *w, *x_scale, *w_scale;
+    const void *bias, *residual;
+    void *y;
+    int64_t m, n, k;
+    int64_t ldx, ldw, ldxs, ldws, ldr, ldy;
+    int32_t scale_type, out_type, act, reserved; /* reserved must be 0 */
+} tg_block_linear_args;
+
+size_t tg_block_linear_workspace_bytes(const tg_block_linear_args *a);
+tg_status tg_block_linear(const tg_block_linear_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
+
+/*
+ * y = x / scale of its block, rounded to TG_E4M3, for x [rows, cols]; a block is 128
+ * consecutive columns (the last one may be shorter) of block_rows rows.
+ *   type        of x: TG_F32, TG_BF16 or TG_F16
+ *   block_rows  1 (tg_block_linear's x) or 128 (its w)
+ *   scale       [ceil(rows / block_rows), ceil(cols / 128)], row stride lds, of
+ *               scale_type: TG_F32, max |x| / 448 over the block's finite values,
+ *               2^-126 at least, and 1 where those are 0; TG_E8M0, the least power of
+ *               two that is no smaller than that
+ * NaN and infinities become NaN.  rows < 2^31, cols < 2^31 - 128.
+ */
+typedef struct {
+    const void *x;
+    void *y, *scale;
+    int64_t rows, cols;
+    int64_t ldx, ldy, lds;
+    int32_t type, scale_type, block_rows, reserved; /* reserved must be 0 */
+} tg_quantize_args;
+
+tg_status tg_quantize(const tg_quantize_args *a, tg_stream stream);
+
+/*
  * h = x + residual (x where residual is NULL), rstd = 1 / sqrt(mean(h^2) + eps)
  * over a row's `cols` elements, y = h rstd weight.
  *   type      of x, residual, weight and hidden: TG_F32, TG_BF16 or TG_F16
@@ -150,6 +250,48 @@ typedef struct {
 
 size_t tg_rms_norm_grad_workspace_bytes(const tg_rms_norm_grad_args *a);
 tg_status tg_rms_norm_grad(const tg_rms_norm_grad_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
+
+/*
+ * h = x + residual (x where residual is NULL), mean = mean(h), rstd = 1 /
+ * sqrt(mean((h - mean)^2) + eps) over a row's `cols` elements, y = (h - mean) rstd
+ * weight + bias.  As tg_rms_norm, but for
+ *   bias        [cols] or NULL, of `type`
+ *   mean        [rows] floats or NULL
+ * The deviations' squares are added after the mean is taken off; rows whose
+ * deviations pass 1.8e19 have rstd 0.
+ */
+typedef struct {
+    const void *x, *residual, *weight, *bias;
+    void *hidden, *y;
+    float *scale, *mean, *rstd;
+    int64_t rows, cols;
+    int64_t ldx, ldr, ldh, ldy;
+    float eps;
+    int32_t type, out_type, reserved; /* reserved must be 0 */
+} tg_layer_norm_args;
+
+tg_status tg_layer_norm(const tg_layer_norm_args *a, tg_stream stream);
+
+/*
+ * Gradients of tg_layer_norm from dy and, where the residual stream goes on,
+ * dhidden (NULL: none): with g = dy weight and n = (h - mean) rstd
+ *   dx = dhidden + rstd (g - mean(g) - n mean(g n)), the gradient of x and of the
+ *        residual alike;  dweight[c] = the sum over rows of dy n,  dbias[c] = that
+ *        of dy (NULL where it is not wanted).
+ * hidden, mean and rstd are tg_layer_norm's; h is read as hidden holds it, rounded.
+ * dx may be dy or dhidden itself.
+ */
+typedef struct {
+    const void *dy, *dhidden, *hidden, *weight;
+    const float *mean, *rstd;
+    void *dx, *dweight, *dbias;
+    int64_t rows, cols;
+    int64_t lddy, lddh, ldh, lddx;
+    int32_t type, reserved; /* reserved must be 0 */
+} tg_layer_norm_grad_args;
+
+size_t tg_layer_norm_grad_workspace_bytes(const tg_layer_norm_grad_args *a);
+tg_status tg_layer_norm_grad(const tg_layer_norm_grad_args *a, void *d_ws, size_t ws_bytes, tg_stream stream);
 
 /*
  * AdamW over many tensors in one launch.  For each element, with g = grad *

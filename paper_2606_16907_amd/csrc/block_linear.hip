@@ -1,0 +1,268 @@
+// block_linear.hip -- matrix product of 8-bit operands with a scale for every 128
+// elements of a row of x and for every 128 x 128 of w (tg_block_linear).
+//
+// With P = x and Q = w, r along their rows, and b the blocks of 128 of r:
+//        C[i][j] = sum over b of ps(i, b) qs(j / 128, b) (sum over r in b of P(i, r) Q(j, r))
+// A block of r is a step of the loop over r, one row of a tile in LDS, and one
+// 16 x 16 x 128 matrix instruction.
+#include "product.h"
+
+namespace tg {
+namespace {
+
+using i32x8 = vec<int, 8>;
+
+// With scales that are powers of two the instruction multiplies by them itself.
+__device__ inline f32x4 mma_block(i32x8 a, i32x8 b, f32x4 c, int code_a, int code_b) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, code_a, 0, code_b);
+}
+__device__ inline f32x4 mma_block(i32x8 a, i32x8 b) { return mma_block(a, b, f32x4(0.0f), 0x7f7f7f7f, 0x7f7f7f7f); }
+
+// The scales of a tile on their way to LDS: groups of four blocks of r, [rows][4]
+// words, of a row 16 bytes.  A load brings 16 rows: lane l the block l % 4 of row
+// l / 4, so that a row's four lie in one access.
+template <bool kPowers>
+struct ScaleStream {
+    static constexpr int kSize = kPowers ? 1 : 4;
+    i32x4 d;
+    int64_t row_bytes;
+    int rows, blocks;  // from here on
+
+    __device__ void init(const void *p, int64_t ld, int64_t row0, int64_t n_rows, int64_t b0, int64_t n_blocks) {
+        row_bytes = ld * kSize;
+        const uint64_t from = (uint64_t)p + row0 * row_bytes + b0 * kSize;
+        rows = (int)std::min<int64_t>(n_rows - row0, 256);
+        blocks = (int)(n_blocks - b0);
+        d[0] = __builtin_amdgcn_readfirstlane((int)from);
+        d[1] = __builtin_amdgcn_readfirstlane((int)(from >> 32) & 0xffff);
+        d[2] = __builtin_amdgcn_readfirstlane((int)((rows - 1) * row_bytes + blocks * kSize));
+        d[3] = 0x00027000;
+    }
+    // Rows row0 .. row0 + 15 of group g, to 256 bytes at `to` of LDS.  What lies past
+    // the last row or block becomes 0.
+    __device__ void load(int g, int row0, unsigned to) const {
+        const int lane = threadIdx.x % 64, row = row0 + lane / 4, b = 4 * g + lane % 4;
+        const int at = row < rows && b < blocks ? (int)(row * row_bytes) + b * kSize : (int)0x80000000;
+        if constexpr (kPowers)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_ubyte %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(d) : "memory");
+        else
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(d) : "memory");
+    }
+};
+
+// 16 kTI kDown x 16 kTJ kAcross of C by kDown x kAcross waves.
+template <typename O, bool kPowers, int kDown, int kAcross, int kTI, int kTJ>
+__global__ __launch_bounds__(64 * kDown * kAcross, 2) void product_blocks(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p,
+                                                                          int64_t r_bytes_q, int share_steps) {
+    constexpr int kWaves = kDown * kAcross, kBI = 16 * kTI * kDown, kBJ = 16 * kTJ * kAcross;
+    constexpr int kTileP = kBI * kStepBytes, kTileQ = kBJ * kStepBytes, kGroup = (kBI + 16) * 16;
+    static_assert(kStepBytes == kScaled, "a step is a block of r");
+    static_assert(kBJ / kScaled <= 16 && kScaled % (16 * kTJ) == 0, "a wave's columns share their scales");
+    __shared__ __attribute__((aligned(1024))) char tiles[2 * kTileP + 2 * kTileQ + 2 * kGroup];
+    int bi, bj;
+    tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
+    const int64_t i0 = (int64_t)bi * kBI, j0 = (int64_t)bj * kBJ;
+    const int wave = wave_index(), lane = threadIdx.x % 64;
+    const int wi = wave / kAcross * 16 * kTI, wj = wave % kAcross * 16 * kTJ;
+    const int64_t r0 = (int64_t)blockIdx.y * share_steps * kScaled, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kScaled);
+    const int steps = (int)((r1 - r0 + kScaled - 1) / kScaled);
+
+    Stream<e4m3, false, kBI, false, kWaves> sp;
+    Stream<e4m3, false, kBJ, false, kWaves> sq;
+    ScaleStream<kPowers> xs, ws;
+    sp.init(a.p, a.ldp, i0, a.ni, r0, r1, r1 < a.nr ? r1 : r_bytes_p);
+    sq.init(a.q, a.ldq, j0, a.nj, r0, r1, r1 < a.nr ? r1 : r_bytes_q);
+    const int64_t b0 = r0 / kScaled;
+    xs.init(a.ps, a.ldps, i0, a.ni, b0, b0 + steps);
+    ws.init(a.qs, a.ldqs, j0 / kScaled, (a.nj + kScaled - 1) / kScaled, b0, b0 + steps);
+    const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)&tiles[0];
+    const unsigned to_p = lds + wave * sp.kLoads * 1024, to_q = lds + 2 * kTileP + wave * sq.kLoads * 1024;
+    constexpr int kScalesAt = 2 * kTileP + 2 * kTileQ;
+    // part `turn` of group g: x's rows in two turns, then w's
+    const auto load_scales = [&](int g, int turn) {
+        const unsigned to = lds + kScalesAt + g % 2 * kGroup;
+        const int rows = (turn * kWaves + wave) * 16;
+        if (rows < kBI) xs.load(g, rows, to + rows * 16);
+        if (turn == 2 && wave == 0) ws.load(g, 0, to + kBI * 16);
+    };
+    const auto load_p = [&](int h) {
+        sp.open(h), sp.settle();
+        each<0, sp.kLoads>([&](auto l) { sp.template load<l>(to_p + h % 2 * kTileP); });
+    };
+    const auto load_q = [&](int h) {
+        sq.open(h), sq.settle();
+        each<0, sq.kLoads>([&](auto l) { sq.template load<l>(to_q + h % 2 * kTileQ); });
+    };
+    f32x4 acc[kTI][kTJ] = {};
+    if (steps > 0) {
+        load_scales(0, 0), load_scales(0, 1), load_scales(0, 2);
+        load_p(0), load_q(0), load_q(1);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(sq.kLoads) : "memory");
+        const int p_at = along_at(wi + lane % 16, lane / 16), q_at = 2 * kTileP + along_at(wj + lane % 16, lane / 16);
+        const int p_at2 = along_at(wi + lane % 16, lane / 16 + 4), q_at2 = 2 * kTileP + along_at(wj + lane % 16, lane / 16 + 4);
+        const auto fragment = [&](int lo, int hi) {
+            return (i32x8)__builtin_shufflevector(*(const i32x4 *)(&tiles[0] + lo), *(const i32x4 *)(&tiles[0] + hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        for (int t = 0; t < steps; ++t) {
+            const int set = t % 2;
+            load_scales(t / 4 + 1, t % 4);
+            load_p(t + 1);
+            i32x8 q[kTJ];
+#pragma unroll
+            for (int y = 0; y < kTJ; ++y) q[y] = fragment(q_at + set * kTileQ + y * 16 * kStepBytes, q_at2 + set * kTileQ + y * 16 * kStepBytes);
+            const int scales_at = kScalesAt + t / 4 % 2 * kGroup + t % 4 * 4;
+            const char *const x_scale = &tiles[0] + scales_at + (wi + lane % 16) * 16;
+            const char *const w_scale = &tiles[0] + scales_at + (kBI + wj / kScaled) * 16;
+            using word = std::conditional_t<kPowers, int, float>;
+            const word sw = *(const word *)w_scale;
+            word s[kTI];
+#pragma unroll
+            for (int x = 0; x < kTI; ++x) s[x] = *(const word *)(x_scale + x * 256);
+            // every wave has what it wants of Q's tile, whose place the one after next takes
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            load_q(t + 2);
+#pragma unroll
+            for (int x = 0; x < kTI; ++x) {
+                const i32x8 p = fragment(p_at + set * kTileP + x * 16 * kStepBytes, p_at2 + set * kTileP + x * 16 * kStepBytes);
+                if constexpr (kPowers) {
+#pragma unroll
+                    for (int y = 0; y < kTJ; ++y) acc[x][y] = mma_block(q[y], p, acc[x][y], sw, s[x]);
+                } else {
+                    const float scale = s[x] * sw;
+                    f32x4 part[kTJ];
+#pragma unroll
+                    for (int y = 0; y < kTJ; ++y) part[y] = mma_block(q[y], p);
+#pragma unroll
+                    for (int y = 0; y < kTJ; ++y) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[x][y][c] = fmaf(part[y][c], scale, acc[x][y][c]);
+                    }
+                }
+            }
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(sq.kLoads) : "memory");
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the last loads, before this LDS has another use
+    }
+    // A lane has columns 4 (lane / 16) + c of row lane % 16 of each 16 x 16 part.  Two
+    // of them at a time go through the wave's share of LDS, in rows 16 bytes longer than
+    // their values, and come back 8 columns a lane.
+    __syncthreads();
+    constexpr int kRow = 16 * kTJ + 4, kUnits = 2 * kTJ, kTurns = 32 * kUnits / 64;
+    static_assert(32 * kRow * 4 * kWaves <= (int)sizeof(tiles), "the waves' shares fit the tiles' place");
+    float *const rows = (float *)&tiles[0] + wave * 32 * kRow;
+    const int col = lane % kUnits * 8;
+    const int64_t j = j0 + wj + col;
+    const int valid = (int)std::min<int64_t>(8, a.nj - j);
+    Columns<8> columns{};
+    if (!e.partial && valid > 0) columns = load_columns<O, 8>(j, valid, e);
+#pragma unroll
+    for (int x = 0; x < kTI; x += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int y = 0; y < kTJ; ++y) *(f32x4 *)(rows + (h * 16 + lane % 16) * kRow + y * 16 + lane / 16 * 4) = acc[x + h][y];
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int n = 0; n < kTurns; ++n) {
+            const int row = n * (64 / kUnits) + lane / kUnits;
+            const int64_t i = i0 + wi + x * 16 + row;
+            if (i >= a.ni || valid <= 0) continue;
+            const f32x4 lo = *(const f32x4 *)(rows + row * kRow + col), hi = *(const f32x4 *)(rows + row * kRow + col + 4);
+            const vec<float, 8> z = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            if (e.partial) {
+                store_f32<float, 8>(e.partial + (blockIdx.y * a.ni + i) * a.nj + j, z, valid);
+            } else {
+                vec<float, 8> residual(0.0f);
+                if (e.residual) residual = load_f32<O, 8>((const O *)e.residual + i * e.ldr + j, valid);
+                finish<O, 8>(z, 1.0f, columns, residual, i, j, valid, e);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <typename O, bool kPowers>
+hipError_t launch_blocks(Product a, Epilogue e, char *ws, hipStream_t s) {
+    constexpr Form kForm = kPowers ? kExponents : kBlocks;
+    if (a.ni == 0 || a.nj == 0) return hipSuccess;
+    int64_t r_bytes_p = a.nr;
+    const Plan p = plan_product<kForm>(a, 1, r_bytes_p, false, false);
+    if (p.few) return launch_few<e4m3, O, kForm>(a, e, p, ws, s);
+    const hipError_t r = pack_operands<e4m3, kForm, false, false>(a, p, r_bytes_p, ws, s);
+    if (r != hipSuccess) return r;
+    const int64_t r_bytes_q = p.pack_q ? a.ldq : a.nr;
+    const Cut &c = p.cut;
+    e.partial = c.splits > 1 ? (float *)(ws + p.p_bytes + p.q_bytes) : nullptr;
+    const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, c.tile);
+    const dim3 grid(ti * tj, c.splits);
+    if (c.tile == 256)
+        hipLaunchKernelGGL((product_blocks<O, kPowers, 2, 4, 8, 4>), grid, dim3(512), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
+    else
+        hipLaunchKernelGGL((product_blocks<O, kPowers, 2, 2, 4, 4>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
+    return join<O, kOne>(a, e, c.splits, s);
+}
+
+Product product_of(const tg_block_linear_args &q) {
+    Product a{q.x, q.w, ld_of(q.ldx, q.m, q.k, TG_E4M3), ld_of(q.ldw, q.n, q.k, TG_E4M3), q.m, q.n, q.k};
+    a.ps = q.x_scale, a.qs = q.w_scale;
+    a.ldps = q.m > 1 ? q.ldxs : 0, a.ldqs = q.n > kScaled ? q.ldws : 0;
+    return a;
+}
+
+// A scale's offset in a tile of 256 rows fits 31 bits.
+constexpr int64_t kMostScaleLd = 1 << 21;
+
+tg_status check_scales(const void *p, int64_t ld, int64_t rows, int64_t cols, int type, const char *what) {
+    if (rows == 0 || cols == 0) return TG_OK;
+    if (!p) return call_failed(TG_EINVAL, "%s is NULL", what);
+    if (type == TG_F32 && (uintptr_t)p % 4) return call_failed(TG_EINVAL, "%s is not aligned to its elements", what);
+    if (rows > 1 && (ld < cols || ld >= kMostScaleLd))
+        return call_failed(TG_EINVAL, "%s: row stride %lld, %lld to %lld expected", what, (long long)ld, (long long)cols, (long long)kMostScaleLd - 1);
+    return TG_OK;
+}
+
+}  // namespace
+}  // namespace tg
+
+using namespace tg;
+
+extern "C" {
+
+size_t tg_block_linear_workspace_bytes(const tg_block_linear_args *q) {
+    if (!q || !sizes_fit(q->m, q->n, q->k)) return 0;
+    return plan_product<kBlocks>(product_of(*q), 1, q->k, false, false).bytes;
+}
+
+tg_status tg_block_linear(const tg_block_linear_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
+    if (!q) return call_failed(TG_EINVAL, "arguments are NULL");
+    if (q->reserved) return call_failed(TG_EINVAL, "reserved must be 0");
+    if (q->scale_type != TG_F32 && q->scale_type != TG_E8M0) return call_failed(TG_EINVAL, "scale_type %d", q->scale_type);
+    if (q->out_type != TG_BF16 && q->out_type != TG_F16) return call_failed(TG_EINVAL, "out_type %d", q->out_type);
+    if (q->act < TG_ACT_NONE || q->act > TG_ACT_GELU) return call_failed(TG_EINVAL, "act %d", q->act);
+    if (!sizes_fit(q->m, q->n, q->k))
+        return call_failed(TG_EINVAL, "m %lld, n %lld, k %lld", (long long)q->m, (long long)q->n, (long long)q->k);
+    const int64_t blocks = ceil_div(q->k, kScaled);
+    TG_TRY(check_matrix(q->x, q->ldx, q->m, q->k, TG_E4M3, "x"));
+    TG_TRY(check_matrix(q->w, q->ldw, q->n, q->k, TG_E4M3, "w"));
+    TG_TRY(check_scales(q->x_scale, q->ldxs, q->m, blocks, q->scale_type, "x_scale"));
+    TG_TRY(check_scales(q->w_scale, q->ldws, ceil_div(q->n, kScaled), blocks, q->scale_type, "w_scale"));
+    TG_TRY(check_matrix(q->y, q->ldy, q->m, q->n, q->out_type, "y"));
+    if (q->residual) TG_TRY(check_matrix(q->residual, q->ldr, q->m, q->n, q->out_type, "residual"));
+    if (q->bias) TG_TRY(check_matrix(q->bias, 0, 1, q->n, q->out_type, "bias"));
+    TG_TRY(check_workspace(d_ws, ws_bytes, tg_block_linear_workspace_bytes(q)));
+    Epilogue e{};
+    e.bias = q->bias, e.residual = q->residual, e.out = q->y;
+    e.ldr = q->ldr, e.ldo = q->ldy, e.act = q->act;
+    const Product a = product_of(*q);
+    const hipStream_t s = (hipStream_t)stream;
+    char *const ws = (char *)d_ws;
+    hipError_t r;
+    if (q->scale_type == TG_F32)
+        r = q->out_type == TG_BF16 ? launch_blocks<bf16, false>(a, e, ws, s) : launch_blocks<f16, false>(a, e, ws, s);
+    else
+        r = q->out_type == TG_BF16 ? launch_blocks<bf16, true>(a, e, ws, s) : launch_blocks<f16, true>(a, e, ws, s);
+    return r == hipSuccess ? TG_OK : device_failed(r, "the block-scaled product");
+}
+
+}  // extern "C"

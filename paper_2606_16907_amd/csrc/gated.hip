@@ -1,0 +1,242 @@
+// gated.hip -- the gated projections of a feed-forward half: gate and up, the
+// activation and their product in one kernel (tg_gated), and their gradients
+// (tg_gated_grad).
+//
+// The products as product.h has them:
+//        y        = act(x wg^T) (x wu^T)    P = x, Q = wg and wu side by side (kGated)
+//        dx       = dg wg + du wu           P = [dg | du], Q = wg, then wu, with r down
+//                                           their columns (kSeam)
+//        dwg, dwu = dg^T x, du^T x          P = [dg | du], Q = x, with r down their
+//                                           columns, C's rows to two outputs (kHalves)
+// Gate and up are never read again for y, and each gradient is one product of twice
+// the size: more tiles at once, and the sums of dx meet in registers.
+#include "product.h"
+
+namespace tg {
+namespace {
+
+// ---------------------------------------------------------------------------
+// dg = dy up act'(gate), du = dy act(gate), and the biases' gradients
+// ---------------------------------------------------------------------------
+struct GatedSlopeArgs {
+    const void *dy, *gate, *up;
+    void *dz;        // [m, 2 half]: dg and du, each padded with zeros to `half` columns; NULL: only the sums
+    float *partial;  // [2][gridDim.y, n] sums of dg's and du's rows, or NULL
+    int64_t m, n, lddy, ldg, ldu, half;
+    int act;
+};
+
+// 256 columns by 8 rows at a time; a block goes down its share of the rows.  dg and
+// du are rounded to the inputs' 16 bits because the matrix instructions of the
+// products read no more; the biases' sums take them before that.  Bound by memory:
+// three matrices read, two written.
+template <typename E>
+__global__ __launch_bounds__(256) void gated_slope_kernel(GatedSlopeArgs a) {
+    using f32x8 = vec<float, 8>;
+    __shared__ float strand[2][8][256 + 8];
+    const int64_t col = (int64_t)blockIdx.x * 256 + (threadIdx.x % 32) * 8;
+    const int g = threadIdx.x / 32;
+    const int valid = (int)std::max<int64_t>(0, std::min<int64_t>(8, a.n - col));
+    const int64_t width = a.dz ? a.half : a.n;
+    f32x8 sum[2] = {f32x8(0.0f), f32x8(0.0f)};
+    if (col < width) {
+        for (int64_t row = (int64_t)blockIdx.y * 8 + g; row < a.m; row += (int64_t)gridDim.y * 8) {
+            const f32x8 dy = load_f32<E, 8>((const E *)a.dy + row * a.lddy + col, valid);
+            const f32x8 gate = load_f32<E, 8>((const E *)a.gate + row * a.ldg + col, valid);
+            const f32x8 up = load_f32<E, 8>((const E *)a.up + row * a.ldu + col, valid);
+            f32x8 d[2], value = gate;
+            d[0] = a.act == TG_ACT_NONE ? dy * up : dy * up * slope<8>(gate, a.act);
+            activate<8>(value, a.act);
+            d[1] = dy * value;
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) d[o][c] = c < valid ? d[o][c] : 0.0f;
+                if (a.dz) store_f32<E, 8>((E *)a.dz + row * 2 * a.half + o * a.half + col, d[o], 8);
+                sum[o] += d[o];
+            }
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) strand[o][g][(threadIdx.x % 32) * 8 + c] = sum[o][c];
+    }
+    __syncthreads();
+    const int64_t out = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (out >= a.n) return;
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+        float total = strand[o][0][threadIdx.x];
+#pragma unroll
+        for (int h = 1; h < 8; ++h) total += strand[o][h][threadIdx.x];
+        a.partial[((int64_t)o * gridDim.y + blockIdx.y) * a.n + out] = total;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+// Columns of dg and of du in their common matrix: whole steps of dx's product.
+int64_t half_of(int64_t n) { return ceil_div(n, 64) * 64; }
+
+bool gated_fits(int64_t m, int64_t n, int64_t k) { return n >= 0 && n <= kMostLd && sizes_fit(m, 2 * half_of(n), k); }
+
+Product forward_product(const tg_gated_args &q) {
+    Product a{q.x, q.w_gate, ld_of(q.ldx, q.m, q.k, q.type), ld_of(q.ldwg, q.n, q.k, q.type), q.m, q.n, q.k};
+    a.q2 = q.w_up, a.ldq2 = ld_of(q.ldwu, q.n, q.k, q.type);
+    return a;
+}
+
+// What tg_gated_grad does, and what lies where in its workspace: dg and du, sums,
+// and the place of the two products, which run one after the other.
+struct GatedGradPlan {
+    bool dz, sums, weights;
+    int64_t half;
+    int rows;
+    size_t dz_bytes, sum_bytes, product_bytes;
+    Product dx, dw;
+    size_t bytes() const { return dz_bytes + sum_bytes + product_bytes; }
+};
+
+GatedGradPlan plan_grad(const tg_gated_grad_args &q, char *ws) {
+    GatedGradPlan p{};
+    p.weights = q.dw_gate || q.dw_up;
+    p.dz = q.dx || p.weights;
+    p.sums = q.dgate_bias || q.dup_bias;
+    p.half = half_of(q.n);
+    p.rows = slope_rows(q.m, q.n);
+    p.dz_bytes = p.dz ? round256((size_t)q.m * 2 * p.half * 2) : 0;
+    p.sum_bytes = p.sums ? round256((size_t)2 * p.rows * q.n * 4) : 0;
+    const int64_t ldz = 2 * p.half;
+    p.dx = Product{ws, q.w_gate, ldz, ld_of(q.ldwg, q.n, q.k, q.type), q.m, q.k, ldz};
+    p.dx.q2 = q.w_up, p.dx.ldq2 = ld_of(q.ldwu, q.n, q.k, q.type), p.dx.seam = p.half, p.dx.half = q.n;
+    // one weight's gradient alone: the first half of the rows, from its columns of dg and du on
+    const bool both = q.dw_gate && q.dw_up;
+    p.dw = Product{ws + (both || q.dw_gate ? 0 : p.half * 2), q.x, ldz, ld_of(q.ldx, q.m, q.k, q.type), both ? ldz : p.half, q.k, q.m};
+    p.dw.seam = p.half, p.dw.half = q.n;
+    if (q.dx) p.product_bytes = plan_product<kSeam>(p.dx, 2, ldz * 2, false, true).bytes;
+    if (p.weights) p.product_bytes = std::max(p.product_bytes, plan_product<kHalves>(p.dw, 2, 0, true, true).bytes);
+    return p;
+}
+
+template <typename E>
+tg_status run_grad(const tg_gated_grad_args &q, const GatedGradPlan &p, char *ws, hipStream_t s) {
+    char *const place = ws + p.dz_bytes + p.sum_bytes;
+    float *const sums = (float *)(ws + p.dz_bytes);
+    if (q.m > 0 && q.n > 0) {
+        GatedSlopeArgs a{q.dy, q.gate, q.up, p.dz ? ws : nullptr, p.sums ? sums : nullptr, q.m, q.n, q.lddy, q.ldg, q.ldu, p.half, q.act};
+        hipLaunchKernelGGL(gated_slope_kernel<E>, dim3((unsigned)ceil_div(p.half, 256), p.rows), dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return device_failed(e, "gated_slope_kernel");
+    }
+    if (p.sums) {
+        const hipError_t e = launch_column_sums_of_two(sums, q.m > 0 ? p.rows : 0, q.n, q.dgate_bias, q.dup_bias, q.type, s);
+        if (e != hipSuccess) return device_failed(e, "column_sums");
+    }
+    if (q.dx) {
+        Epilogue e{};
+        e.out = q.dx, e.ldo = q.lddx;
+        const hipError_t r = launch_product<E, E, false, true, kSeam>(p.dx, e, p.dx.ldp * 2, place, s);
+        if (r != hipSuccess) return device_failed(r, "the product dg wg + du wu");
+    }
+    if (p.weights) {
+        Epilogue e{};
+        e.out = q.dw_gate ? q.dw_gate : q.dw_up, e.ldo = q.dw_gate ? q.lddwg : q.lddwu;
+        e.out2 = q.dw_up, e.ldo2 = q.lddwu;
+        const hipError_t r = launch_product<E, E, true, true, kHalves>(p.dw, e, 0, place, s);
+        if (r != hipSuccess) return device_failed(r, "the products dg^T x and du^T x");
+    }
+    return TG_OK;
+}
+
+}  // namespace
+}  // namespace tg
+
+using namespace tg;
+
+extern "C" {
+
+size_t tg_gated_workspace_bytes(const tg_gated_args *q) {
+    if (!q || !valid_types(q->type, q->out_type) || !gated_fits(q->m, q->n, q->k)) return 0;
+    const int size = (int)size_of(q->type);
+    return plan_product<kGated>(forward_product(*q), size, q->k * size, false, false).bytes;
+}
+
+tg_status tg_gated(const tg_gated_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
+    if (!q) return call_failed(TG_EINVAL, "arguments are NULL");
+    if (q->reserved) return call_failed(TG_EINVAL, "reserved must be 0");
+    if (!valid_types(q->type, q->out_type)) return call_failed(TG_EINVAL, "type %d with out_type %d", q->type, q->out_type);
+    if (q->act < TG_ACT_NONE || q->act > TG_ACT_GELU) return call_failed(TG_EINVAL, "act %d", q->act);
+    if (!gated_fits(q->m, q->n, q->k))
+        return call_failed(TG_EINVAL, "m %lld, n %lld, k %lld", (long long)q->m, (long long)q->n, (long long)q->k);
+    const bool scaled = q->x_scale != nullptr;
+    if ((q->gate_scale != nullptr) != scaled || (q->up_scale != nullptr) != scaled || (scaled && q->type != TG_E4M3))
+        return call_failed(TG_EINVAL, "x_scale, gate_scale and up_scale come together, with 8-bit inputs");
+    if ((q->gate != nullptr) != (q->up != nullptr)) return call_failed(TG_EINVAL, "gate and up are kept together");
+    TG_TRY(check_matrix(q->x, q->ldx, q->m, q->k, q->type, "x"));
+    TG_TRY(check_matrix(q->w_gate, q->ldwg, q->n, q->k, q->type, "w_gate"));
+    TG_TRY(check_matrix(q->w_up, q->ldwu, q->n, q->k, q->type, "w_up"));
+    TG_TRY(check_matrix(q->y, q->ldy, q->m, q->n, q->out_type, "y"));
+    if (q->gate) TG_TRY(check_matrix(q->gate, q->ldg, q->m, q->n, q->out_type, "gate"));
+    if (q->up) TG_TRY(check_matrix(q->up, q->ldu, q->m, q->n, q->out_type, "up"));
+    if (q->gate_bias) TG_TRY(check_matrix(q->gate_bias, 0, 1, q->n, q->out_type, "gate_bias"));
+    if (q->up_bias) TG_TRY(check_matrix(q->up_bias, 0, 1, q->n, q->out_type, "up_bias"));
+    if (scaled) {
+        TG_TRY(check_matrix(q->x_scale, 0, 1, q->m, TG_F32, "x_scale"));
+        TG_TRY(check_matrix(q->gate_scale, 0, 1, q->n, TG_F32, "gate_scale"));
+        TG_TRY(check_matrix(q->up_scale, 0, 1, q->n, TG_F32, "up_scale"));
+    }
+    TG_TRY(check_workspace(d_ws, ws_bytes, tg_gated_workspace_bytes(q)));
+    const Product a = forward_product(*q);
+    Epilogue e{};
+    e.x_scale = q->x_scale, e.w_scale = q->gate_scale, e.w_scale2 = q->up_scale;
+    e.bias = q->gate_bias, e.bias2 = q->up_bias;
+    e.out = q->y, e.pre = q->gate, e.pre2 = q->up;
+    e.ldo = q->ldy, e.ldp = q->ldg, e.ldp2 = q->ldu, e.act = q->act;
+    const hipStream_t s = (hipStream_t)stream;
+    char *const ws = (char *)d_ws;
+    hipError_t r;
+    if (q->type == TG_BF16)
+        r = launch_product<bf16, bf16, false, false, kGated>(a, e, q->k * 2, ws, s);
+    else if (q->type == TG_F16)
+        r = launch_product<f16, f16, false, false, kGated>(a, e, q->k * 2, ws, s);
+    else if (q->out_type == TG_BF16)
+        r = launch_product<e4m3, bf16, false, false, kGated>(a, e, q->k, ws, s);
+    else
+        r = launch_product<e4m3, f16, false, false, kGated>(a, e, q->k, ws, s);
+    return r == hipSuccess ? TG_OK : device_failed(r, "the gated products");
+}
+
+size_t tg_gated_grad_workspace_bytes(const tg_gated_grad_args *q) {
+    if (!q || !gated_fits(q->m, q->n, q->k)) return 0;
+    return plan_grad(*q, nullptr).bytes();
+}
+
+tg_status tg_gated_grad(const tg_gated_grad_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
+    if (!q) return call_failed(TG_EINVAL, "arguments are NULL");
+    if (q->type != TG_BF16 && q->type != TG_F16) return call_failed(TG_EINVAL, "type %d", q->type);
+    if (q->act < TG_ACT_NONE || q->act > TG_ACT_GELU) return call_failed(TG_EINVAL, "act %d", q->act);
+    if (!gated_fits(q->m, q->n, q->k))
+        return call_failed(TG_EINVAL, "m %lld, n %lld, k %lld", (long long)q->m, (long long)q->n, (long long)q->k);
+    TG_TRY(check_matrix(q->dy, q->lddy, q->m, q->n, q->type, "dy"));
+    TG_TRY(check_matrix(q->gate, q->ldg, q->m, q->n, q->type, "gate"));
+    TG_TRY(check_matrix(q->up, q->ldu, q->m, q->n, q->type, "up"));
+    if (q->dw_gate || q->dw_up) TG_TRY(check_matrix(q->x, q->ldx, q->m, q->k, q->type, "x"));
+    if (q->dw_gate) TG_TRY(check_matrix(q->dw_gate, q->lddwg, q->n, q->k, q->type, "dw_gate"));
+    if (q->dw_up) TG_TRY(check_matrix(q->dw_up, q->lddwu, q->n, q->k, q->type, "dw_up"));
+    if (q->dx) {
+        TG_TRY(check_matrix(q->w_gate, q->ldwg, q->n, q->k, q->type, "w_gate"));
+        TG_TRY(check_matrix(q->w_up, q->ldwu, q->n, q->k, q->type, "w_up"));
+        TG_TRY(check_matrix(q->dx, q->lddx, q->m, q->k, q->type, "dx"));
+    }
+    if (q->dgate_bias) TG_TRY(check_matrix(q->dgate_bias, 0, 1, q->n, q->type, "dgate_bias"));
+    if (q->dup_bias) TG_TRY(check_matrix(q->dup_bias, 0, 1, q->n, q->type, "dup_bias"));
+    const GatedGradPlan p = plan_grad(*q, (char *)d_ws);
+    TG_TRY(check_workspace(d_ws, ws_bytes, p.bytes()));
+    return q->type == TG_BF16 ? run_grad<bf16>(*q, p, (char *)d_ws, (hipStream_t)stream)
+                              : run_grad<f16>(*q, p, (char *)d_ws, (hipStream_t)stream);
+}
+
+}  // extern "C"

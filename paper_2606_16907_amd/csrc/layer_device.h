@@ -93,6 +93,27 @@ __device__ inline void store_f32(T *p, vec<float, N> r, int valid) {
 }
 
 constexpr float kE4M3Max = 448.0f;
+constexpr float kLeastScale = 0x1p-126f;  // of an 8-bit output: the least normal number
+
+template <typename E>
+constexpr int kUnitOf = 16 / sizeof(E);  // elements in 16 bytes
+
+template <int kUnit>
+__device__ inline void store_e4m3(unsigned char *p, vec<float, kUnit> q, int valid) {
+    vec<unsigned, kUnit / 4> w;
+#pragma unroll
+    for (int h = 0; h < kUnit / 4; ++h) {
+        int t = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], 0, false);
+        w[h] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], t, true);
+    }
+    if (valid >= kUnit) {
+        reinterpret_cast<Loose<vec<unsigned, kUnit / 4>, 1> *>(p)->v = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e)
+            if (e < valid) p[e] = (unsigned char)(w[e / 4] >> (8 * (e % 4)));
+    }
+}
 
 __device__ inline bool finite_f32(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 // |x| where x is a number below infinity, else 0.
@@ -141,5 +162,7 @@ __device__ inline float block_reduce(float x, float *slots) {
 // out[c] = the sum of partial[r][c] over rows r (reduce.hip: ascending r within
 // eight interleaved strands, then the strands in order).
 hipError_t launch_column_sums(const float *partial, int rows, int64_t cols, void *out, int type, hipStream_t s);
+// The same of two tables, one behind the other; an output that is NULL is left out.
+hipError_t launch_column_sums_of_two(const float *partial, int rows, int64_t cols, void *out, void *out2, int type, hipStream_t s);
 
 }  // namespace tg

@@ -1,0 +1,453 @@
+// norm.h -- norms over rows with the residual's addition, and their gradients: the
+// kernels of rms_norm.hip (kCentre false) and layer_norm.hip (kCentre true).
+//
+// Both are bound by memory: forward reads x and residual and writes hidden and
+// y, backward reads dy, hidden and dhidden and writes dx, each once, so a row
+// stays in registers between its statistic and its output.  A row is cut into
+// units of 16 bytes; thread t of the row's T threads holds units t, t + T, ...
+// (N of them), every load of the row in flight before the reduction.  8192 x 8192
+// in bf16 takes 89 us forward (6.0 TB/s), as much with 8 bits out, and 117
+// backward (4.6 TB/s), where a large copy reaches 4.8 to 4.9; forward with 256
+// threads a row took 96, backward with 768 or 1024 blocks 24 and 11 more in all,
+// with the next row fetched ahead the same.  The gradient of short rows is bound
+// by latency instead: its 512 blocks have a wave each up to 64 units a row, and
+// 16384 x 512 in bf16 takes 47 us, 1.4 TB/s.
+//
+// hidden is h rounded once to the inputs' type, which is what the next operator
+// and the gradient read; y is of the h before that rounding.  In 16 bits with a
+// residual the gradients so carry the error of one rounding beside their own.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+
+#include "layer_device.h"
+
+namespace tg {
+namespace {
+
+struct NormArgs {
+    const void *x, *residual, *weight, *bias;
+    void *hidden, *y;
+    float *scale, *mean, *rstd;
+    int64_t rows, ldx, ldr, ldh, ldy;
+    int64_t first;  // row of block 0
+    int cols;
+    float eps, inv_cols;
+};
+
+__device__ inline int left_of(int cols, int col) { return cols - col; }  // <= 0: none
+
+// Both reductions at once, in the order of block_reduce.
+struct Two {
+    float a, b;
+};
+template <int T>
+__device__ inline Two block_sums(Two x, Two *slots) {
+    x.a = wave_reduce<OpSum>(x.a), x.b = wave_reduce<OpSum>(x.b);
+    if (T == 64) return x;
+    if (threadIdx.x % 64 == 0) slots[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = slots[0];
+#pragma unroll
+    for (int w = 1; w < T / 64; ++w) x.a += slots[w].a, x.b += slots[w].b;
+    return x;
+}
+
+// kCentre: the row's mean is taken off first, and the bias added at the end.  The
+// second pass over the registers corrects the first one's mean by what is left of
+// the row around it, so a row far from 0 keeps its deviations.
+// One row per T threads, N units a thread (T N units or fewer), 256 / T rows a block
+// where T is 64.  kStream: rows of any length, read again for each pass (x and
+// residual add up to the same h every time), one row a block.
+template <typename E, bool kEight, int T, int N, bool kStream, bool kCentre>
+__global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
+    constexpr int kRows = T == 64 ? 4 : 1;
+    __shared__ float slots[2][T / 64];
+    __shared__ Two pairs[T / 64];
+    const int t = threadIdx.x % T;
+    const int64_t row = a.first + (int64_t)blockIdx.x * kRows + threadIdx.x / T;
+    if (kRows > 1 && row >= a.rows) return;  // whole waves, which meet no barrier
+    const E *const x = (const E *)a.x + row * a.ldx;
+    const E *const r = a.residual ? (const E *)a.residual + row * a.ldr : nullptr;
+    E *const hidden = a.hidden ? (E *)a.hidden + row * a.ldh : nullptr;
+    const E *const weight = (const E *)a.weight, *const bias = (const E *)a.bias;
+
+    const auto read = [&](int col) {
+        const int valid = left_of(a.cols, col);
+        unit h = load_f32<E, kUnit>(x + col, valid);
+        if (r) h += load_f32<E, kUnit>(r + col, valid);
+        return h;
+    };
+    const auto write = [&](int col, unit y, float scale) {
+        const int valid = left_of(a.cols, col);
+        if (kEight) {
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) y[e] /= scale;
+            store_e4m3<kUnit>((unsigned char *)a.y + row * a.ldy + col, y, valid);
+        } else {
+            store_f32<E, kUnit>((E *)a.y + row * a.ldy + col, y, valid);
+        }
+    };
+
+    unit h[N];
+    const int units = (a.cols + kUnit - 1) / kUnit;
+    // f(h, valid elements of it) over the thread's units
+    const auto over = [&](auto f) {
+        if (kStream) {
+            for (int u = t; u < units; u += T) f(read(u * kUnit), left_of(a.cols, u * kUnit));
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) f(h[n], t + n * T < units ? left_of(a.cols, (t + n * T) * kUnit) : 0);
+        }
+    };
+    if (!kStream) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) h[n] = t + n * T < units ? read((t + n * T) * kUnit) : unit(0.0f);
+    }
+    float squares = 0.0f, mean = 0.0f;
+    if constexpr (kCentre) {
+        float sum = 0.0f;
+        over([&](unit v, int) {
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) sum += v[e];
+        });
+        mean = block_reduce<OpSum, T>(sum, slots[0]) * a.inv_cols;
+        Two two{0.0f, 0.0f};
+        over([&](unit v, int valid) {
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) {
+                const float d = e < valid ? v[e] - mean : 0.0f;
+                two.a += d, two.b = fmaf(d, d, two.b);
+            }
+        });
+        two = block_sums<T>(two, pairs);
+        const float off = two.a * a.inv_cols;
+        squares = fmaxf(fmaf(-two.a, off, two.b), two.b * 0.0f);  // not below 0; NaN stays
+        mean += off;
+        if (a.mean && t == 0) a.mean[row] = mean;
+    } else {
+        over([&](unit v, int) {
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) squares = fmaf(v[e], v[e], squares);
+        });
+        squares = block_reduce<OpSum, T>(squares, slots[0]);
+    }
+    const float rstd = 1.0f / sqrtf(fmaf(squares, a.inv_cols, a.eps));
+    if (a.rstd && t == 0) a.rstd[row] = rstd;
+
+    const auto normed = [&](unit v, int col) {
+        const unit w = load_f32<E, kUnit>(weight + col, left_of(a.cols, col));
+        unit y;
+        if constexpr (kCentre) {
+            unit b(0.0f);
+            if (bias) b = load_f32<E, kUnit>(bias + col, left_of(a.cols, col));
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) y[e] = fmaf((v[e] - mean) * rstd, w[e], b[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) y[e] = (v[e] * rstd) * w[e];
+        }
+        return y;
+    };
+    float scale = 1.0f;
+    if (kEight) {
+        float most = 0.0f;
+        if (kStream) {
+            for (int u = t; u < units; u += T) {
+                const unit y = normed(read(u * kUnit), u * kUnit);
+#pragma unroll
+                for (int e = 0; e < kUnit; ++e) most = fmaxf(most, finite_abs(y[e]));  // past the row's end weight and bias are 0
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int u = t + n * T;
+                if (u >= units) continue;
+                if (hidden) store_f32<E, kUnit>(hidden + u * kUnit, h[n], left_of(a.cols, u * kUnit));
+                h[n] = normed(h[n], u * kUnit);
+#pragma unroll
+                for (int e = 0; e < kUnit; ++e) most = fmaxf(most, finite_abs(h[n][e]));
+            }
+        }
+        most = block_reduce<OpMax, T>(most, slots[1]);
+        // a subnormal scale has few bits, and a row's largest over it could pass 448
+        scale = most > 0.0f ? fmaxf(most / kE4M3Max, kLeastScale) : 1.0f;
+        if (t == 0) a.scale[row] = scale;
+    }
+    if (kStream) {
+        for (int u = t; u < units; u += T) {
+            const unit v = read(u * kUnit);
+            // hidden may be x or residual: this unit was just read for the last time
+            if (hidden) store_f32<E, kUnit>(hidden + u * kUnit, v, left_of(a.cols, u * kUnit));
+            write(u * kUnit, normed(v, u * kUnit), scale);
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int u = t + n * T;
+            if (u >= units) continue;
+            if (!kEight && hidden) store_f32<E, kUnit>(hidden + u * kUnit, h[n], left_of(a.cols, u * kUnit));
+            write(u * kUnit, kEight ? h[n] : normed(h[n], u * kUnit), scale);
+        }
+    }
+}
+
+struct GradArgs {
+    const void *dy, *dhidden, *hidden, *weight;
+    const float *mean, *rstd;
+    void *dx;
+    float *partial;   // [gridDim.x, cols] sums of dy h rstd
+    float *partial2;  // those of dy, or NULL
+    int64_t rows, lddy, lddh, ldh, lddx;
+    int64_t first;  // of block 0: its unit of columns (norm_grad_weight_stream), its row (norm_grad_stream)
+    int cols;
+    float inv_cols;
+};
+
+// A block takes rows blockIdx.x, + gridDim.x, ... and keeps its columns' share of
+// dweight in registers over all of them; one row of sums a block leaves it.  The
+// weight stays in registers too, except in blocks of 1024, whose threads have 128.
+template <typename E, int T, int N, bool kCentre>
+__global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
+    __shared__ float slots[2][T / 64];
+    __shared__ Two pairs[2][T / 64];
+    const int t = threadIdx.x;
+    const int units = (a.cols + kUnit - 1) / kUnit;
+    constexpr bool kKeep = T < 1024;
+    unit kept[N], dw[N], db[N];
+    const auto weight = [&](int n) {
+        const int u = t + n * T;
+        return u < units ? load_f32<E, kUnit>((const E *)a.weight + u * kUnit, left_of(a.cols, u * kUnit)) : unit(0.0f);
+    };
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        dw[n] = db[n] = unit(0.0f);
+        if (kKeep) kept[n] = weight(n);
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const E *const dy = (const E *)a.dy + row * a.lddy;
+        const E *const hidden = (const E *)a.hidden + row * a.ldh;
+        const E *const dh = a.dhidden ? (const E *)a.dhidden + row * a.lddh : nullptr;
+        unit g[N], h[N], more[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int u = t + n * T, valid = u < units ? left_of(a.cols, u * kUnit) : 0;
+            g[n] = h[n] = more[n] = unit(0.0f);
+            if (u >= units) continue;
+            g[n] = load_f32<E, kUnit>(dy + u * kUnit, valid);
+            h[n] = load_f32<E, kUnit>(hidden + u * kUnit, valid);
+            if (dh) more[n] = load_f32<E, kUnit>(dh + u * kUnit, valid);
+        }
+        const float rstd = a.rstd[row], centre = kCentre ? a.mean[row] : 0.0f;
+        float dot = 0.0f, sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const unit w = kKeep ? kept[n] : weight(n);
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) {
+                const float xhat = (kCentre ? h[n][e] - centre : h[n][e]) * rstd;
+                dw[n][e] = fmaf(g[n][e], xhat, dw[n][e]);
+                if (kCentre) db[n][e] += g[n][e];
+                g[n][e] *= w[e];
+                h[n][e] = xhat;
+                dot = fmaf(g[n][e], xhat, dot);
+                if (kCentre) sum += g[n][e];
+            }
+        }
+        // the slots of the row before last are free: a barrier lies between
+        float mean, lift = 0.0f;
+        if constexpr (kCentre) {
+            const Two two = block_sums<T>(Two{dot, sum}, pairs[turn]);
+            mean = two.a * a.inv_cols, lift = two.b * a.inv_cols;
+        } else {
+            mean = block_reduce<OpSum, T>(dot, slots[turn]) * a.inv_cols;
+        }
+        E *const dx = (E *)a.dx + row * a.lddx;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int u = t + n * T;
+            if (u >= units) continue;
+            unit d;
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) d[e] = fmaf(rstd, fmaf(-h[n][e], mean, kCentre ? g[n][e] - lift : g[n][e]), more[n][e]);
+            store_f32<E, kUnit>(dx + u * kUnit, d, left_of(a.cols, u * kUnit));
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int u = t + n * T;
+        if (u >= units) continue;
+        const int64_t at = (int64_t)blockIdx.x * a.cols + u * kUnit;
+        store_f32<float, kUnit>(a.partial + at, dw[n], left_of(a.cols, u * kUnit));
+        if (kCentre && a.partial2) store_f32<float, kUnit>(a.partial2 + at, db[n], left_of(a.cols, u * kUnit));
+    }
+}
+
+// Rows too long for registers: dweight's sums first, while dy is whole (dx may
+// be dy), a thread a unit of columns and a block a share of the rows ...
+template <typename E, bool kCentre>
+__global__ __launch_bounds__(256) void norm_grad_weight_stream(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
+    const int64_t u = a.first + (int64_t)blockIdx.y * 256 + threadIdx.x;
+    if (u * kUnit >= a.cols) return;
+    const int col = (int)u * kUnit, valid = left_of(a.cols, col);
+    unit dw(0.0f), db(0.0f);
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const unit g = load_f32<E, kUnit>((const E *)a.dy + row * a.lddy + col, valid);
+        const unit h = load_f32<E, kUnit>((const E *)a.hidden + row * a.ldh + col, valid);
+        const float rstd = a.rstd[row], centre = kCentre ? a.mean[row] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) dw[e] = fmaf(g[e], (kCentre ? h[e] - centre : h[e]) * rstd, dw[e]);
+        if (kCentre) db += g;
+    }
+    store_f32<float, kUnit>(a.partial + (int64_t)blockIdx.x * a.cols + col, dw, valid);
+    if (kCentre && a.partial2) store_f32<float, kUnit>(a.partial2 + (int64_t)blockIdx.x * a.cols + col, db, valid);
+}
+// ... then dx, a row a block, read twice.
+template <typename E, bool kCentre>
+__global__ __launch_bounds__(1024) void norm_grad_stream(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
+    __shared__ float slots[16];
+    __shared__ Two pairs[16];
+    const int64_t row = a.first + blockIdx.x;
+    const int units = (a.cols + kUnit - 1) / kUnit;
+    const E *const dy = (const E *)a.dy + row * a.lddy;
+    const E *const hidden = (const E *)a.hidden + row * a.ldh;
+    const E *const dh = a.dhidden ? (const E *)a.dhidden + row * a.lddh : nullptr;
+    E *const dx = (E *)a.dx + row * a.lddx;
+    const float rstd = a.rstd[row], centre = kCentre ? a.mean[row] : 0.0f;
+    float dot = 0.0f, sum = 0.0f;
+    for (int u = threadIdx.x; u < units; u += 1024) {
+        const int col = u * kUnit, valid = left_of(a.cols, col);
+        const unit g = load_f32<E, kUnit>(dy + col, valid), h = load_f32<E, kUnit>(hidden + col, valid);
+        const unit w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) {
+            dot = fmaf(g[e] * w[e], (kCentre ? h[e] - centre : h[e]) * rstd, dot);
+            if (kCentre) sum = fmaf(g[e], w[e], sum);
+        }
+    }
+    float mean, lift = 0.0f;
+    if constexpr (kCentre) {
+        const Two two = block_sums<1024>(Two{dot, sum}, pairs);
+        mean = two.a * a.inv_cols, lift = two.b * a.inv_cols;
+    } else {
+        mean = block_reduce<OpSum, 1024>(dot, slots) * a.inv_cols;
+    }
+    for (int u = threadIdx.x; u < units; u += 1024) {
+        const int col = u * kUnit, valid = left_of(a.cols, col);
+        const unit g = load_f32<E, kUnit>(dy + col, valid), h = load_f32<E, kUnit>(hidden + col, valid);
+        const unit w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
+        unit d(0.0f);
+        if (dh) d = load_f32<E, kUnit>(dh + col, valid);
+#pragma unroll
+        for (int e = 0; e < kUnit; ++e) {
+            const float xhat = (kCentre ? h[e] - centre : h[e]) * rstd;
+            d[e] = fmaf(rstd, fmaf(-xhat, mean, kCentre ? g[e] * w[e] - lift : g[e] * w[e]), d[e]);
+        }
+        store_f32<E, kUnit>(dx + col, d, valid);
+    }
+}
+
+constexpr int64_t kMostBlocks = 1 << 20;  // of a launch: a grid holds fewer than 2^32 threads
+
+template <typename E, bool kEight, bool kCentre>
+hipError_t launch_norm(NormArgs a, hipStream_t s) {
+    const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
+    const auto go = [&](auto kernel, int threads, int rows_per_block) {
+        for (a.first = 0; a.first < a.rows; a.first += kMostBlocks * rows_per_block) {
+            const int64_t blocks = std::min(kMostBlocks, ceil_div(a.rows - a.first, rows_per_block));
+            hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, a);
+        }
+    };
+    // A wave a row while a row is at most two units a lane; beyond that 256 to
+    // 1024 threads with one or two units each, and four only in rows of more than
+    // 2048 units.  Few rows leave most of the chip idle whatever is done, so
+    // they take more threads a row.
+    if (units <= 64)
+        go(norm_kernel<E, kEight, 64, 1, false, kCentre>, 256, 4);
+    else if (units <= 128)
+        go(norm_kernel<E, kEight, 64, 2, false, kCentre>, 256, 4);
+    else if (units <= 256)
+        go(norm_kernel<E, kEight, 256, 1, false, kCentre>, 256, 1);
+    else if (units <= 512 && a.rows >= 256)
+        go(norm_kernel<E, kEight, 256, 2, false, kCentre>, 256, 1);
+    else if (units <= 1024 && a.rows >= 256)
+        go(norm_kernel<E, kEight, 512, 2, false, kCentre>, 512, 1);
+    else if (units <= 1024)
+        go(norm_kernel<E, kEight, 1024, 1, false, kCentre>, 1024, 1);
+    else if (units <= 2048)
+        go(norm_kernel<E, kEight, 1024, 2, false, kCentre>, 1024, 1);
+    else if (units <= 4096)
+        go(norm_kernel<E, kEight, 1024, 4, false, kCentre>, 1024, 1);
+    else
+        go(norm_kernel<E, kEight, 1024, 1, true, kCentre>, 1024, 1);
+    return hipGetLastError();
+}
+
+// Blocks of the gradient: each leaves a row of sums, so no more than fill the
+// chip a few times over.
+inline int grad_blocks(int64_t rows) { return (int)(rows < 512 ? rows : 512); }
+
+template <typename E, bool kCentre>
+hipError_t launch_grad(GradArgs a, hipStream_t s) {
+    const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
+    const dim3 grid((unsigned)grad_blocks(a.rows));
+    const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a); };
+    constexpr int kMost = kUnitOf<E> == 4 ? 4096 : 2048;  // units of a row that stays in registers
+    if (units <= 64) {
+        go(norm_grad_kernel<E, 64, 1, kCentre>, 64);
+    } else if (units <= 256) {
+        go(norm_grad_kernel<E, 256, 1, kCentre>, 256);
+    } else if (units <= 512) {
+        go(norm_grad_kernel<E, 256, 2, kCentre>, 256);
+    } else if (units <= 1024) {
+        go(norm_grad_kernel<E, 512, 2, kCentre>, 512);
+    } else if (units <= 2048) {
+        go(norm_grad_kernel<E, 1024, 2, kCentre>, 1024);
+    } else if (units <= kMost) {
+        go(norm_grad_kernel<E, 1024, kMost / 1024, kCentre>, 1024);
+    } else {
+        constexpr int64_t kMostUnits = 1 << 20;  // of a launch: 2^12 blocks across the columns by 512 down the rows
+        for (; a.first < units; a.first += kMostUnits) {
+            const dim3 blocks(grid.x, (unsigned)ceil_div(std::min(kMostUnits, units - a.first), 256));
+            hipLaunchKernelGGL((norm_grad_weight_stream<E, kCentre>), blocks, dim3(256), 0, s, a);
+        }
+        for (a.first = 0; a.first < a.rows; a.first += kMostBlocks)
+            hipLaunchKernelGGL((norm_grad_stream<E, kCentre>), dim3((unsigned)std::min(kMostBlocks, a.rows - a.first)), dim3(1024), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+inline size_t size_of(int type) { return type == TG_F32 ? 4 : type == TG_E4M3 ? 1 : 2; }
+inline bool norm_type(int type) { return type == TG_F32 || type == TG_BF16 || type == TG_F16; }
+
+inline tg_status check_rows(const void *p, int64_t ld, int64_t rows, int64_t cols, int type, const char *what) {
+    if (!p) return call_failed(TG_EINVAL, "%s is NULL", what);
+    if ((uintptr_t)p % size_of(type)) return call_failed(TG_EINVAL, "%s is not aligned to its elements", what);
+    if (rows > 1 && ld < cols) return call_failed(TG_EINVAL, "%s: row stride %lld below the row length %lld", what, (long long)ld, (long long)cols);
+    return TG_OK;
+}
+
+inline tg_status check_sizes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || rows > 0x7fffffff || cols > 0x7fffffff - 64)
+        return call_failed(TG_EINVAL, "rows %lld, cols %lld", (long long)rows, (long long)cols);
+    return TG_OK;
+}
+
+#define TG_TRY(call)                  \
+    do {                              \
+        const tg_status st_ = (call); \
+        if (st_ != TG_OK) return st_; \
+    } while (0)
+
+}  // namespace
+}  // namespace tg

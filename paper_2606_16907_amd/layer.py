@@ -6,6 +6,11 @@ half of a planned layer on one GPU.
     f = tg_rms_norm(x, weight, residual=r)              # f.y, f.hidden, f.rstd
     q = tg_rms_norm(x, weight, residual=r, out_dtype=torch.float8_e4m3fn)
     y = tg_linear(q.y, w8, x_scale=q.scale, w_scale=w8_scale)
+    y, gate, up = tg_gated(x, w_gate, w_up, act="silu", keep_pre=True)
+    g = tg_gated_grad(dy, x, w_gate, w_up, gate, up, act="silu")    # g.dx, g.dw_gate, g.dw_up
+    q, w8 = tg_quantize(x), tg_quantize(w, block_rows=128)
+    y = tg_block_linear(q.y, w8.y, q.scale, w8.scale, residual=r)
+    f = tg_layer_norm(x, weight, bias=b, residual=r)    # f.y, f.hidden, f.mean, f.rstd
     opt = AdamW(params, grads, *adamw_states(params, bits=8), masters=masters)
     opt.step(step, lr=1e-4, seed=step)
 
@@ -26,10 +31,12 @@ import torch
 
 from . import tangram as T
 
-E4M3 = torch.float8_e4m3fn
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, E4M3: 3}
+SCALE_TYPES = {torch.float32: 0, E8M0: 4}
 ACTS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 SCALE_BLOCK = 256  # consecutive elements of an 8-bit optimizer state that share a scale
+BLOCK = 128  # columns (and rows of a weight) of 8-bit values that share a scale
 
 _vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 
@@ -47,12 +54,29 @@ TgRmsNormArgs = _struct("TgRmsNormArgs", p=("x residual weight hidden y scale rs
                         t=("type out_type reserved", _i32))
 TgRmsNormGradArgs = _struct("TgRmsNormGradArgs", p=("dy dhidden hidden weight rstd dx dweight", _vp),
                             n=("rows cols lddy lddh ldh lddx", _i64), t=("type reserved", _i32))
+TgGatedArgs = _struct("TgGatedArgs", p=("x w_gate w_up x_scale gate_scale up_scale gate_bias up_bias y gate up", _vp),
+                      n=("m n k ldx ldwg ldwu ldy ldg ldu", _i64), t=("type out_type act reserved", _i32))
+TgGatedGradArgs = _struct("TgGatedGradArgs",
+                          p=("dy gate up x w_gate w_up dx dw_gate dw_up dgate_bias dup_bias", _vp),
+                          n=("m n k lddy ldg ldu ldx ldwg ldwu lddx lddwg lddwu", _i64), t=("type act", _i32))
+TgBlockLinearArgs = _struct("TgBlockLinearArgs", p=("x w x_scale w_scale bias residual y", _vp),
+                            n=("m n k ldx ldw ldxs ldws ldr ldy", _i64), t=("scale_type out_type act reserved", _i32))
+TgQuantizeArgs = _struct("TgQuantizeArgs", p=("x y scale", _vp), n=("rows cols ldx ldy lds", _i64),
+                         t=("type scale_type block_rows reserved", _i32))
+TgLayerNormArgs = _struct("TgLayerNormArgs", p=("x residual weight bias hidden y scale mean rstd", _vp),
+                          n=("rows cols ldx ldr ldh ldy", _i64), e=("eps", ctypes.c_float),
+                          t=("type out_type reserved", _i32))
+TgLayerNormGradArgs = _struct("TgLayerNormGradArgs", p=("dy dhidden hidden weight mean rstd dx dweight dbias", _vp),
+                              n=("rows cols lddy lddh ldh lddx", _i64), t=("type reserved", _i32))
 TgAdamwTensor = _struct("TgAdamwTensor", p=("param grad master m v m_scale v_scale", _vp), n=("n", _i64))
 TgAdamwRates = _struct("TgAdamwRates", r=("lr beta1 beta2 eps weight_decay grad_scale", ctypes.c_double),
                        n=("step", _i64), t=("seed reserved", ctypes.c_uint32))
 
 EXPORTS = ("tg_linear_workspace_bytes", "tg_linear", "tg_linear_grad_workspace_bytes", "tg_linear_grad",
+           "tg_gated_workspace_bytes", "tg_gated", "tg_gated_grad_workspace_bytes", "tg_gated_grad",
+           "tg_block_linear_workspace_bytes", "tg_block_linear", "tg_quantize",
            "tg_rms_norm", "tg_rms_norm_grad_workspace_bytes", "tg_rms_norm_grad",
+           "tg_layer_norm", "tg_layer_norm_grad_workspace_bytes", "tg_layer_norm_grad",
            "tg_adamw_create", "tg_adamw_step", "tg_adamw_destroy")
 
 _lib = None
@@ -66,11 +90,15 @@ def load_library():
     L = T.load_library()
     P = ctypes.POINTER
     for name, args in (("tg_linear", TgLinearArgs), ("tg_linear_grad", TgLinearGradArgs),
-                       ("tg_rms_norm_grad", TgRmsNormGradArgs)):
+                       ("tg_gated", TgGatedArgs), ("tg_gated_grad", TgGatedGradArgs),
+                       ("tg_block_linear", TgBlockLinearArgs),
+                       ("tg_rms_norm_grad", TgRmsNormGradArgs), ("tg_layer_norm_grad", TgLayerNormGradArgs)):
         size = getattr(L, name + "_workspace_bytes")
         size.argtypes, size.restype = [P(args)], _sz
         getattr(L, name).argtypes = [P(args), _vp, _sz, _vp]
     L.tg_rms_norm.argtypes = [P(TgRmsNormArgs), _vp]
+    L.tg_layer_norm.argtypes = [P(TgLayerNormArgs), _vp]
+    L.tg_quantize.argtypes = [P(TgQuantizeArgs), _vp]
     L.tg_adamw_create.argtypes = [P(TgAdamwTensor), _i32, _i32, _i32, _i32, P(_vp)]
     L.tg_adamw_step.argtypes = [_vp, P(TgAdamwRates), _vp]
     L.tg_adamw_destroy.argtypes, L.tg_adamw_destroy.restype = [_vp], None
@@ -213,6 +241,140 @@ def tg_linear_grad(dy, x, w, pre=None, act="none", bias_grad=False, x_grad=True,
     return dx, dw, db
 
 
+def tg_gated(x, w_gate, w_up, gate_bias=None, up_bias=None, act="silu", x_scale=None, gate_scale=None, up_scale=None,
+             out_dtype=None, keep_pre=False, out=None, workspace=None):
+    """act(gate) up with gate = x w_gate^T + gate_bias and up = x w_up^T + up_bias
+    for x [m, k] and w_gate, w_up [n, k] in bfloat16, float16 or float8_e4m3fn
+    (then x_scale [m], gate_scale [n] and up_scale [n] floats multiply the
+    products, all or none, and the other operands have out_dtype, bfloat16 unless
+    given).  Returns y, or with keep_pre (y, gate, up): what tg_gated_grad wants."""
+    lib = load_library()
+    device = torch.cuda.current_device()
+    dtype = x.dtype
+    if dtype not in TYPES or dtype == torch.float32:
+        raise ValueError(f"x: dtype {dtype}, bfloat16, float16 or float8_e4m3fn expected")
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if dtype == E4M3 else dtype
+    if (out_dtype not in (torch.bfloat16, torch.float16)) or (dtype != E4M3 and out_dtype != dtype):
+        raise ValueError(f"out_dtype: {out_dtype} for inputs of {dtype}")
+    px, ldx = _matrix(x, dtype, None, None, "x", device)
+    m, k = x.shape
+    pg, ldwg = _matrix(w_gate, dtype, None, k, "w_gate", device)
+    n = w_gate.shape[0]
+    pu, ldwu = _matrix(w_up, dtype, n, k, "w_up", device)
+    scales = (x_scale, gate_scale, up_scale)
+    if any(s is not None for s in scales) and (dtype != E4M3 or any(s is None for s in scales)):
+        raise ValueError("x_scale, gate_scale and up_scale come together, with 8-bit inputs")
+    psx, psg, psu = (None if s is None else _vector(s, torch.float32, size, what, device)
+                     for s, size, what in zip(scales, (m, n, n), ("x_scale", "gate_scale", "up_scale")))
+    pbg, pbu = (None if b is None else _vector(b, out_dtype, n, what, device)
+                for b, what in ((gate_bias, "gate_bias"), (up_bias, "up_bias")))
+    act = _act(act)
+    y, py, ldy = _out(out, x, m, n, out_dtype, device)
+    gate, pgate, ldg = _out(None, x, m, n, out_dtype, device) if keep_pre else (None, None, 0)
+    up, pup, ldu = _out(None, x, m, n, out_dtype, device) if keep_pre else (None, None, 0)
+    a = TgGatedArgs(px, pg, pu, psx, psg, psu, pbg, pbu, py, pgate, pup, m, n, k, ldx, ldwg, ldwu, ldy, ldg, ldu,
+                    TYPES[dtype], TYPES[out_dtype], act, 0)
+    ws, size, _kept = _workspace(lib.tg_gated_workspace_bytes(a), workspace, x, device)
+    T._check(lib.tg_gated(a, ws, size, _stream(device)), "tg_gated")
+    return (y, gate, up) if keep_pre else y
+
+
+class GatedGrads(NamedTuple):
+    dx: Optional[torch.Tensor]
+    dw_gate: Optional[torch.Tensor]
+    dw_up: Optional[torch.Tensor]
+    dgate_bias: Optional[torch.Tensor]
+    dup_bias: Optional[torch.Tensor]
+
+
+def tg_gated_grad(dy, x, w_gate, w_up, gate, up, act="silu", bias_grad=False, x_grad=True, w_grad=True, dx=None,
+                  dw_gate=None, dw_up=None, dgate_bias=None, dup_bias=None, workspace=None):
+    """Gradients of tg_gated from dy [m, n], in the inputs' type; those not asked
+    for are None, those given are written to.  `gate` and `up` are tg_gated's."""
+    lib = load_library()
+    device = torch.cuda.current_device()
+    dtype = dy.dtype
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"dy: dtype {dtype}, bfloat16 or float16 expected")
+    pdy, lddy = _matrix(dy, dtype, None, None, "dy", device)
+    m, n = dy.shape
+    px, ldx = _matrix(x, dtype, m, None, "x", device)
+    k = x.shape[1]
+    pwg, ldwg = _matrix(w_gate, dtype, n, k, "w_gate", device)
+    pwu, ldwu = _matrix(w_up, dtype, n, k, "w_up", device)
+    pg, ldg = _matrix(gate, dtype, m, n, "gate", device)
+    pu, ldu = _matrix(up, dtype, m, n, "up", device)
+    act = _act(act)
+    dx, pdx, lddx = _out(dx, dy, m, k, dtype, device, "dx") if x_grad else (None, None, 0)
+    dwg, pdwg, lddwg = _out(dw_gate, dy, n, k, dtype, device, "dw_gate") if w_grad else (None, None, 0)
+    dwu, pdwu, lddwu = _out(dw_up, dy, n, k, dtype, device, "dw_up") if w_grad else (None, None, 0)
+    dbg, pdbg = _vector_out(dgate_bias, dy, n, device, "dgate_bias") if bias_grad else (None, None)
+    dbu, pdbu = _vector_out(dup_bias, dy, n, device, "dup_bias") if bias_grad else (None, None)
+    a = TgGatedGradArgs(pdy, pg, pu, px, pwg, pwu, pdx, pdwg, pdwu, pdbg, pdbu, m, n, k, lddy, ldg, ldu, ldx, ldwg, ldwu,
+                        lddx, lddwg, lddwu, TYPES[dtype], act)
+    ws, size, _kept = _workspace(lib.tg_gated_grad_workspace_bytes(a), workspace, dy, device)
+    T._check(lib.tg_gated_grad(a, ws, size, _stream(device)), "tg_gated_grad")
+    return GatedGrads(dx, dwg, dwu, dbg, dbu)
+
+
+class Quantized(NamedTuple):
+    y: torch.Tensor      # float8_e4m3fn
+    scale: torch.Tensor  # [ceil(rows / block_rows), ceil(cols / 128)]
+
+
+def tg_quantize(x, block_rows=1, scale_dtype=torch.float32, out=None, scale=None):
+    """8-bit values of float32, bfloat16 or float16 rows with a scale for every 128
+    consecutive columns of a row (block_rows 1) or of 128 rows (block_rows 128):
+    max |x| / 448 over the block, or with scale_dtype float8_e8m0fnu the least
+    power of two that is no smaller.  `out` and `scale` are written to where given."""
+    lib = load_library()
+    device = torch.cuda.current_device()
+    dtype = x.dtype
+    if dtype not in TYPES or dtype == E4M3:
+        raise ValueError(f"x: dtype {dtype}, float32, bfloat16 or float16 expected")
+    if scale_dtype not in SCALE_TYPES:
+        raise ValueError(f"scale_dtype: {scale_dtype}, float32 or float8_e8m0fnu expected")
+    if block_rows not in (1, BLOCK):
+        raise ValueError(f"block_rows: {block_rows}, 1 or {BLOCK} expected")
+    px, ldx = _matrix(x, dtype, None, None, "x", device)
+    rows, cols = x.shape
+    y, py, ldy = _out(out, x, rows, cols, E4M3, device)
+    scale, ps, lds = _out(scale, x, -(-rows // block_rows), -(-cols // BLOCK), scale_dtype, device, "scale")
+    a = TgQuantizeArgs(px, py, ps, rows, cols, ldx, ldy, lds, TYPES[dtype], SCALE_TYPES[scale_dtype], block_rows, 0)
+    T._check(lib.tg_quantize(a, _stream(device)), "tg_quantize")
+    return Quantized(y, scale)
+
+
+def tg_block_linear(x, w, x_scale, w_scale, bias=None, act="none", residual=None, out_dtype=torch.bfloat16, out=None,
+                    workspace=None):
+    """act(x w^T + bias) + residual for float8_e4m3fn x [m, k] and w [n, k], x with a
+    scale for every 128 columns of a row, x_scale [m, ceil(k / 128)], and w for
+    every block of 128 x 128, w_scale [ceil(n / 128), ceil(k / 128)], both float32
+    or both float8_e8m0fnu.  The other operands have out_dtype, bfloat16 or
+    float16.  `out` receives y and may be the residual."""
+    lib = load_library()
+    device = torch.cuda.current_device()
+    if x_scale.dtype not in SCALE_TYPES:
+        raise ValueError(f"x_scale: dtype {x_scale.dtype}, float32 or float8_e8m0fnu expected")
+    if out_dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"out_dtype: {out_dtype}, bfloat16 or float16 expected")
+    px, ldx = _matrix(x, E4M3, None, None, "x", device)
+    m, k = x.shape
+    pw, ldw = _matrix(w, E4M3, None, k, "w", device)
+    n, blocks = w.shape[0], -(-k // BLOCK)
+    pxs, ldxs = _matrix(x_scale, x_scale.dtype, m, blocks, "x_scale", device)
+    pws, ldws = _matrix(w_scale, x_scale.dtype, -(-n // BLOCK), blocks, "w_scale", device)
+    pb = None if bias is None else _vector(bias, out_dtype, n, "bias", device)
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, out_dtype, m, n, "residual", device)
+    y, py, ldy = _out(out, x, m, n, out_dtype, device)
+    a = TgBlockLinearArgs(px, pw, pxs, pws, pb, pr, py, m, n, k, ldx, ldw, ldxs, ldws, ldr, ldy,
+                          SCALE_TYPES[x_scale.dtype], TYPES[out_dtype], _act(act), 0)
+    ws, size, _kept = _workspace(lib.tg_block_linear_workspace_bytes(a), workspace, x, device)
+    T._check(lib.tg_block_linear(a, ws, size, _stream(device)), "tg_block_linear")
+    return y
+
+
 class Norm(NamedTuple):
     y: torch.Tensor
     scale: Optional[torch.Tensor]  # [rows], 8-bit outputs only
@@ -272,6 +434,72 @@ def tg_rms_norm_grad(dy, hidden, weight, rstd, dhidden=None, dx=None, dweight=No
     ws, size, _kept = _workspace(lib.tg_rms_norm_grad_workspace_bytes(a), workspace, dy, device)
     T._check(lib.tg_rms_norm_grad(a, ws, size, _stream(device)), "tg_rms_norm_grad")
     return dx, dweight
+
+
+class LayerNorm(NamedTuple):
+    y: torch.Tensor
+    scale: Optional[torch.Tensor]  # [rows], 8-bit outputs only
+    hidden: torch.Tensor           # x + residual; x itself where there is no residual
+    mean: Optional[torch.Tensor]   # [rows], for the gradient
+    rstd: Optional[torch.Tensor]   # the same
+
+
+def tg_layer_norm(x, weight, bias=None, residual=None, eps=1e-5, out_dtype=None, out=None, keep_stats=None):
+    """h = x + residual, y = (h - mean(h)) / sqrt(mean((h - mean(h))^2) + eps) *
+    weight + bias over rows of float32, bfloat16 or float16; with out_dtype
+    float8_e4m3fn y is y / scale for a scale per row.  mean and rstd, which the
+    gradient takes, are returned with outputs in the inputs' type, or as keep_stats
+    says."""
+    lib = load_library()
+    device = torch.cuda.current_device()
+    dtype = x.dtype
+    if dtype not in TYPES or dtype == E4M3:
+        raise ValueError(f"x: dtype {dtype}, float32, bfloat16 or float16 expected")
+    if out_dtype is None:
+        out_dtype = dtype
+    if out_dtype not in (dtype, E4M3):
+        raise ValueError(f"out_dtype: {out_dtype} for an input of {dtype}")
+    px, ldx = _matrix(x, dtype, None, None, "x", device)
+    rows, cols = x.shape
+    pw = _vector(weight, dtype, cols, "weight", device)
+    pb = None if bias is None else _vector(bias, dtype, cols, "bias", device)
+    pr, ldr = (None, 0) if residual is None else _matrix(residual, dtype, rows, cols, "residual", device)
+    eight = out_dtype == E4M3
+    hidden, ph, ldh = (x, None, 0) if residual is None else _out(None, x, rows, cols, dtype, device)
+    y, py, ldy = _out(out, x, rows, cols, out_dtype, device)
+    scale = x.new_empty(rows, dtype=torch.float32) if eight else None
+    keep = keep_stats or (keep_stats is None and not eight)
+    mean, rstd = (x.new_empty(rows, dtype=torch.float32) if keep else None for _ in range(2))
+    a = TgLayerNormArgs(px, pr, pw, pb, ph, py, *(None if t is None else t.data_ptr() for t in (scale, mean, rstd)), rows,
+                        cols, ldx, ldr, ldh, ldy, eps, TYPES[dtype], TYPES[out_dtype], 0)
+    T._check(lib.tg_layer_norm(a, _stream(device)), "tg_layer_norm")
+    return LayerNorm(y, scale, hidden, mean, rstd)
+
+
+def tg_layer_norm_grad(dy, hidden, weight, mean, rstd, dhidden=None, bias_grad=True, dx=None, dweight=None, dbias=None,
+                       workspace=None):
+    """(dx, dweight, dbias) of tg_layer_norm, dbias None where it is not asked for;
+    dx is the gradient of x and of the residual alike.  dhidden is the gradient that
+    arrives at `hidden` from further on; outputs are written to where they are given
+    (dx may be dy or dhidden)."""
+    lib = load_library()
+    device = torch.cuda.current_device()
+    dtype = dy.dtype
+    if dtype not in TYPES or dtype == E4M3:
+        raise ValueError(f"dy: dtype {dtype}, float32, bfloat16 or float16 expected")
+    pdy, lddy = _matrix(dy, dtype, None, None, "dy", device)
+    rows, cols = dy.shape
+    ph, ldh = _matrix(hidden, dtype, rows, cols, "hidden", device)
+    pw = _vector(weight, dtype, cols, "weight", device)
+    pm, ps = (_vector(t, torch.float32, rows, what, device) for t, what in ((mean, "mean"), (rstd, "rstd")))
+    pdh, lddh = (None, 0) if dhidden is None else _matrix(dhidden, dtype, rows, cols, "dhidden", device)
+    dx, pdx, lddx = _out(dx, dy, rows, cols, dtype, device, "dx")
+    dweight, pdw = _vector_out(dweight, dy, cols, device, "dweight")
+    dbias, pdb = _vector_out(dbias, dy, cols, device, "dbias") if bias_grad else (None, None)
+    a = TgLayerNormGradArgs(pdy, pdh, ph, pw, pm, ps, pdx, pdw, pdb, rows, cols, lddy, lddh, ldh, lddx, TYPES[dtype], 0)
+    ws, size, _kept = _workspace(lib.tg_layer_norm_grad_workspace_bytes(a), workspace, dy, device)
+    T._check(lib.tg_layer_norm_grad(a, ws, size, _stream(device)), "tg_layer_norm_grad")
+    return dx, dweight, dbias
 
 
 # ----------------------------------------------------------------------------
