@@ -2,6 +2,168 @@
 // gradient (tg_layer_norm_grad); the kernels are norm.h's.
 #include "norm.h"
 
+namespace tg {
+namespace {
+
+// 16 bytes of a row as they lie; elements at or past `valid` are 0 and not read.
+template <typename E>
+__device__ inline i32x4 load_bits(const E *p, int valid) {
+    if (valid >= kUnitOf<E>) return ((const Global<Loose<i32x4, alignof(E)>> *)p)->v;
+    i32x4 r(0);
+#pragma unroll
+    for (int e = 0; e < kUnitOf<E>; ++e) {
+        if (e >= valid) continue;
+        if constexpr (sizeof(E) == 4)
+            r[e] = ((const Global<int> *)p)[e];
+        else
+            r[e / 2] |= (int)((unsigned)((const Global<unsigned short> *)p)[e] << (16 * (e % 2)));
+    }
+    return r;
+}
+template <typename E>
+__device__ inline vec<float, kUnitOf<E>> floats(i32x4 bits) {
+    return __builtin_convertvector(__builtin_bit_cast(vec<E, kUnitOf<E>>, bits), vec<float, kUnitOf<E>>);
+}
+// The compiler does not know from here on what the bits became before.
+__device__ inline void forget(i32x4 &bits) { asm volatile("" : "+v"(bits)); }
+
+// dx, and a row of sums for dweight and dbias from each block.  T threads have a row;
+// with T = 64 a block has kRows of them at a time, else one.  A row stays in 16-byte
+// units as it was read, converted in both passes over it, so that there is room for
+// the next row, on its way meanwhile (kAhead); the sums of a thread's columns stay in registers over all rows.
+template <typename E, int T, int N, int kRows, bool kAhead>
+__global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a) {
+    constexpr int kUnit = kUnitOf<E>;
+    using unit = vec<float, kUnit>;
+    static_assert(T == 64 || kRows == 1, "rows that meet at barriers have a block of their own");
+    __shared__ unit sums[2][T == 64 ? N * 64 : 1];
+    __shared__ Two pairs[2][T / 64];
+    const int t = threadIdx.x % T, units = (a.cols + kUnit - 1) / kUnit;
+    i32x4 weight[N];
+    unit dw[N], db[N];
+    const auto valid = [&](int n) { return t + n * T < units ? left_of(a.cols, (t + n * T) * kUnit) : 0; };
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        weight[n] = load_bits<E>((const E *)a.weight + (t + n * T) * kUnit, valid(n));
+        dw[n] = db[n] = unit(0.0f);
+    }
+    struct Row {
+        i32x4 g[N], h[N], more[N];
+        float mean, rstd;
+    };
+    const auto fetch = [&](Row &r, int64_t row) {
+        const E *const dy = (const E *)a.dy + row * a.lddy, *const hidden = (const E *)a.hidden + row * a.ldh;
+        const E *const dh = a.dhidden ? (const E *)a.dhidden + row * a.lddh : nullptr;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int col = (t + n * T) * kUnit, left = valid(n);
+            r.g[n] = load_bits<E>(dy + col, left);
+            r.h[n] = load_bits<E>(hidden + col, left);
+            r.more[n] = dh ? load_bits<E>(dh + col, left) : i32x4(0);
+        }
+        r.mean = a.mean[row], r.rstd = a.rstd[row];
+    };
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / T;
+    Row now;
+    if (kAhead && row < a.rows) fetch(now, row);
+    for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
+        Row next;
+        if (!kAhead)
+            fetch(now, row);
+        else if (row + step < a.rows)
+            fetch(next, row + step);
+        Two two{0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const unit g = floats<E>(now.g[n]), h = floats<E>(now.h[n]), w = floats<E>(weight[n]);
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) {
+                const float xhat = (h[e] - now.mean) * now.rstd, gw = g[e] * w[e];
+                dw[n][e] = fmaf(g[e], xhat, dw[n][e]);
+                db[n][e] += g[e];
+                two.a += gw;
+                two.b = fmaf(gw, xhat, two.b);
+            }
+            forget(now.g[n]), forget(now.h[n]), forget(weight[n]);
+            __builtin_amdgcn_sched_barrier(0);  // a unit's floats at a time
+        }
+        // the pairs of the row before last are free: a barrier lies between
+        two = block_sums<T>(two, pairs[turn]);
+        const float lift = two.a * a.inv_cols, mean = two.b * a.inv_cols;
+        E *const dx = (E *)a.dx + row * a.lddx;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int left = valid(n);
+            if (left <= 0) continue;
+            const unit g = floats<E>(now.g[n]), h = floats<E>(now.h[n]), w = floats<E>(weight[n]), more = floats<E>(now.more[n]);
+            unit d;
+#pragma unroll
+            for (int e = 0; e < kUnit; ++e) {
+                const float xhat = (h[e] - now.mean) * now.rstd;
+                d[e] = fmaf(now.rstd, fmaf(-xhat, mean, fmaf(g[e], w[e], -lift)), more[e]);
+            }
+            store_f32<E, kUnit>(dx + (t + n * T) * kUnit, d, left);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (kAhead) now = next;
+    }
+    if constexpr (T == 64) {  // the rows of a block, in order
+        for (int r = 0; r < kRows; ++r) {
+            if ((int)threadIdx.x / T == r) {
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    if (r) dw[n] = sums[0][n * 64 + t] + dw[n], db[n] = sums[1][n * 64 + t] + db[n];
+                    sums[0][n * 64 + t] = dw[n], sums[1][n * 64 + t] = db[n];
+                }
+            }
+            __syncthreads();
+        }
+        if ((int)threadIdx.x / T != kRows - 1) return;
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int64_t at = (int64_t)blockIdx.x * a.cols + (t + n * T) * kUnit;
+        if (valid(n) <= 0) continue;
+        store_f32<float, kUnit>(a.partial + at, dw[n], valid(n));
+        if (a.partial2) store_f32<float, kUnit>(a.partial2 + at, db[n], valid(n));
+    }
+}
+
+// Blocks of the gradient: each leaves a row of sums for the weight and one for the
+// bias.
+int layer_grad_blocks(int64_t rows, int64_t cols, int type) {
+    const int64_t units = ceil_div(cols * (type == TG_F32 ? 4 : 2), 16);
+    const int64_t most = units <= 128 ? ceil_div(rows, 8) : rows;
+    return (int)std::min<int64_t>(most, units <= 1024 || units > 2048 ? 512 : 256);
+}
+
+template <typename E>
+hipError_t launch_layer_grad(GradArgs a, int blocks, hipStream_t s) {
+    const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
+    const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, s, a); };
+    if (units <= 64)
+        go(layer_norm_grad_kernel<E, 64, 1, 8, true>, 512);
+    else if (units <= 128)
+        go(layer_norm_grad_kernel<E, 64, 2, 8, true>, 512);
+    else if (units <= 256)
+        go(layer_norm_grad_kernel<E, 256, 1, 1, true>, 256);
+    else if (units <= 512)
+        go(layer_norm_grad_kernel<E, 256, 2, 1, true>, 256);
+    else if (units <= 1024)
+        go(layer_norm_grad_kernel<E, 512, 2, 1, true>, 512);
+    else if (units <= 1536)
+        go(layer_norm_grad_kernel<E, 768, 2, 1, true>, 768);
+    else if (units <= 2048)
+        go(layer_norm_grad_kernel<E, 1024, 2, 1, false>, 1024);
+    else
+        launch_grad_stream<E, true>(a, blocks, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace tg
+
 using namespace tg;
 
 extern "C" {
@@ -44,7 +206,7 @@ tg_status tg_layer_norm(const tg_layer_norm_args *q, tg_stream stream) {
 
 size_t tg_layer_norm_grad_workspace_bytes(const tg_layer_norm_grad_args *q) {
     if (!q || q->rows < 0 || q->cols < 0 || q->rows > 0x7fffffff || q->cols > 0x7fffffff - 64) return 0;
-    return round256((size_t)grad_blocks(q->rows) * q->cols * (q->dbias ? 8 : 4));
+    return round256((size_t)layer_grad_blocks(q->rows, q->cols, q->type) * q->cols * (q->dbias ? 8 : 4));
 }
 
 tg_status tg_layer_norm_grad(const tg_layer_norm_grad_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
@@ -70,16 +232,17 @@ tg_status tg_layer_norm_grad(const tg_layer_norm_grad_args *q, void *d_ws, size_
         if (ws_bytes < need || !d_ws) return call_failed(TG_ENOMEM, "workspace of %zu bytes, %zu needed", d_ws ? ws_bytes : 0, need);
         const bool one = q->rows == 1;
         float *const sums = (float *)d_ws;
+        const int blocks = layer_grad_blocks(q->rows, q->cols, q->type);
         GradArgs a{q->dy, q->dhidden, q->hidden, q->weight, q->mean, q->rstd, q->dx, sums,
-                   q->dbias ? sums + (int64_t)grad_blocks(q->rows) * q->cols : nullptr, q->rows,
+                   q->dbias ? sums + (int64_t)blocks * q->cols : nullptr, q->rows,
                    one ? 0 : q->lddy, one ? 0 : q->lddh, one ? 0 : q->ldh, one ? 0 : q->lddx,
                    0, (int)q->cols, (float)(1.0 / (double)q->cols)};
-        e = q->type == TG_F32    ? launch_grad<float, true>(a, s)
-            : q->type == TG_BF16 ? launch_grad<bf16, true>(a, s)
-                                 : launch_grad<f16, true>(a, s);
+        e = q->type == TG_F32    ? launch_layer_grad<float>(a, blocks, s)
+            : q->type == TG_BF16 ? launch_layer_grad<bf16>(a, blocks, s)
+                                 : launch_layer_grad<f16>(a, blocks, s);
         if (e != hipSuccess) return device_failed(e, "norm_grad_kernel");
     }
-    e = launch_column_sums_of_two((const float *)d_ws, grad_blocks(q->rows), q->cols, q->dweight, q->dbias, q->type, s);
+    e = launch_column_sums_of_two((const float *)d_ws, layer_grad_blocks(q->rows, q->cols, q->type), q->cols, q->dweight, q->dbias, q->type, s);
     return e == hipSuccess ? TG_OK : device_failed(e, "column_sums");
 }
 

@@ -207,88 +207,6 @@ struct GradArgs {
     float inv_cols;
 };
 
-// A block takes rows blockIdx.x, + gridDim.x, ... and keeps its columns' share of
-// dweight in registers over all of them; one row of sums a block leaves it.  The
-// weight stays in registers too, except in blocks of 1024, whose threads have 128.
-template <typename E, int T, int N, bool kCentre>
-__global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
-    constexpr int kUnit = kUnitOf<E>;
-    using unit = vec<float, kUnit>;
-    __shared__ float slots[2][T / 64];
-    __shared__ Two pairs[2][T / 64];
-    const int t = threadIdx.x;
-    const int units = (a.cols + kUnit - 1) / kUnit;
-    constexpr bool kKeep = T < 1024;
-    unit kept[N], dw[N], db[N];
-    const auto weight = [&](int n) {
-        const int u = t + n * T;
-        return u < units ? load_f32<E, kUnit>((const E *)a.weight + u * kUnit, left_of(a.cols, u * kUnit)) : unit(0.0f);
-    };
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        dw[n] = db[n] = unit(0.0f);
-        if (kKeep) kept[n] = weight(n);
-    }
-    int turn = 0;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const E *const dy = (const E *)a.dy + row * a.lddy;
-        const E *const hidden = (const E *)a.hidden + row * a.ldh;
-        const E *const dh = a.dhidden ? (const E *)a.dhidden + row * a.lddh : nullptr;
-        unit g[N], h[N], more[N];
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int u = t + n * T, valid = u < units ? left_of(a.cols, u * kUnit) : 0;
-            g[n] = h[n] = more[n] = unit(0.0f);
-            if (u >= units) continue;
-            g[n] = load_f32<E, kUnit>(dy + u * kUnit, valid);
-            h[n] = load_f32<E, kUnit>(hidden + u * kUnit, valid);
-            if (dh) more[n] = load_f32<E, kUnit>(dh + u * kUnit, valid);
-        }
-        const float rstd = a.rstd[row], centre = kCentre ? a.mean[row] : 0.0f;
-        float dot = 0.0f, sum = 0.0f;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const unit w = kKeep ? kept[n] : weight(n);
-#pragma unroll
-            for (int e = 0; e < kUnit; ++e) {
-                const float xhat = (kCentre ? h[n][e] - centre : h[n][e]) * rstd;
-                dw[n][e] = fmaf(g[n][e], xhat, dw[n][e]);
-                if (kCentre) db[n][e] += g[n][e];
-                g[n][e] *= w[e];
-                h[n][e] = xhat;
-                dot = fmaf(g[n][e], xhat, dot);
-                if (kCentre) sum += g[n][e];
-            }
-        }
-        // the slots of the row before last are free: a barrier lies between
-        float mean, lift = 0.0f;
-        if constexpr (kCentre) {
-            const Two two = block_sums<T>(Two{dot, sum}, pairs[turn]);
-            mean = two.a * a.inv_cols, lift = two.b * a.inv_cols;
-        } else {
-            mean = block_reduce<OpSum, T>(dot, slots[turn]) * a.inv_cols;
-        }
-        E *const dx = (E *)a.dx + row * a.lddx;
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int u = t + n * T;
-            if (u >= units) continue;
-            unit d;
-#pragma unroll
-            for (int e = 0; e < kUnit; ++e) d[e] = fmaf(rstd, fmaf(-h[n][e], mean, kCentre ? g[n][e] - lift : g[n][e]), more[n][e]);
-            store_f32<E, kUnit>(dx + u * kUnit, d, left_of(a.cols, u * kUnit));
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int u = t + n * T;
-        if (u >= units) continue;
-        const int64_t at = (int64_t)blockIdx.x * a.cols + u * kUnit;
-        store_f32<float, kUnit>(a.partial + at, dw[n], left_of(a.cols, u * kUnit));
-        if (kCentre && a.partial2) store_f32<float, kUnit>(a.partial2 + at, db[n], left_of(a.cols, u * kUnit));
-    }
-}
-
 // Rows too long for registers: dweight's sums first, while dy is whole (dx may
 // be dy), a thread a unit of columns and a block a share of the rows ...
 template <typename E, bool kCentre>
@@ -384,6 +302,10 @@ hipError_t launch_norm(NormArgs a, hipStream_t s) {
         go(norm_kernel<E, kEight, 512, 2, false, kCentre>, 512, 1);
     else if (units <= 1024)
         go(norm_kernel<E, kEight, 1024, 1, false, kCentre>, 1024, 1);
+    else if (kCentre && units <= 1536 && a.rows >= 256 && sizeof(E) == 2)  // 8192 x 12288: 153 us, by 768 threads 164
+        go(norm_kernel<E, kEight, 512, 3, false, kCentre>, 512, 1);
+    else if (kCentre && units <= 1536)  // 3001 x 4999 of floats: 41.5 us, by 512 threads 45.5
+        go(norm_kernel<E, kEight, 768, 2, false, kCentre>, 768, 1);
     else if (units <= 2048)
         go(norm_kernel<E, kEight, 1024, 2, false, kCentre>, 1024, 1);
     else if (units <= 4096)
@@ -393,38 +315,17 @@ hipError_t launch_norm(NormArgs a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Blocks of the gradient: each leaves a row of sums, so no more than fill the
-// chip a few times over.
-inline int grad_blocks(int64_t rows) { return (int)(rows < 512 ? rows : 512); }
-
+// Rows too long for registers: `blocks` down the rows leave a row of sums each.
 template <typename E, bool kCentre>
-hipError_t launch_grad(GradArgs a, hipStream_t s) {
+void launch_grad_stream(GradArgs a, int blocks, hipStream_t s) {
     const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
-    const dim3 grid((unsigned)grad_blocks(a.rows));
-    const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a); };
-    constexpr int kMost = kUnitOf<E> == 4 ? 4096 : 2048;  // units of a row that stays in registers
-    if (units <= 64) {
-        go(norm_grad_kernel<E, 64, 1, kCentre>, 64);
-    } else if (units <= 256) {
-        go(norm_grad_kernel<E, 256, 1, kCentre>, 256);
-    } else if (units <= 512) {
-        go(norm_grad_kernel<E, 256, 2, kCentre>, 256);
-    } else if (units <= 1024) {
-        go(norm_grad_kernel<E, 512, 2, kCentre>, 512);
-    } else if (units <= 2048) {
-        go(norm_grad_kernel<E, 1024, 2, kCentre>, 1024);
-    } else if (units <= kMost) {
-        go(norm_grad_kernel<E, 1024, kMost / 1024, kCentre>, 1024);
-    } else {
-        constexpr int64_t kMostUnits = 1 << 20;  // of a launch: 2^12 blocks across the columns by 512 down the rows
-        for (; a.first < units; a.first += kMostUnits) {
-            const dim3 blocks(grid.x, (unsigned)ceil_div(std::min(kMostUnits, units - a.first), 256));
-            hipLaunchKernelGGL((norm_grad_weight_stream<E, kCentre>), blocks, dim3(256), 0, s, a);
-        }
-        for (a.first = 0; a.first < a.rows; a.first += kMostBlocks)
-            hipLaunchKernelGGL((norm_grad_stream<E, kCentre>), dim3((unsigned)std::min(kMostBlocks, a.rows - a.first)), dim3(1024), 0, s, a);
+    constexpr int64_t kMostUnits = 1 << 20;  // of a launch: 2^12 blocks across the columns by 512 down the rows
+    for (; a.first < units; a.first += kMostUnits) {
+        const dim3 grid(blocks, (unsigned)ceil_div(std::min(kMostUnits, units - a.first), 256));
+        hipLaunchKernelGGL((norm_grad_weight_stream<E, kCentre>), grid, dim3(256), 0, s, a);
     }
-    return hipGetLastError();
+    for (a.first = 0; a.first < a.rows; a.first += kMostBlocks)
+        hipLaunchKernelGGL((norm_grad_stream<E, kCentre>), dim3((unsigned)std::min(kMostBlocks, a.rows - a.first)), dim3(1024), 0, s, a);
 }
 
 inline size_t size_of(int type) { return type == TG_F32 ? 4 : type == TG_E4M3 ? 1 : 2; }
