@@ -65,19 +65,20 @@ struct ScaleStream {
     __device__ void advance() { tg::advance(d, 4 * kSize); }
 };
 
-// A wave's sums to C, from row i0 and column j0 on.  A lane has columns 4 (lane / 16) +
+// A wave's sums to C, from row i0 and column j0 on, or where they are a share's to
+// `part`, rows of `ld`.  A lane has columns 4 (lane / 16) +
 // c of row lane % 16 of each 16 x 16 part.  Two of them at a time go through the
 // wave's place in LDS, in rows 16 bytes longer than their values, and come back 8
 // columns a lane.
 template <typename O, int kTI, int kTJ>
-__device__ inline void finish_blocks(const f32x4 (&acc)[kTI][kTJ], float *rows, const Product &a, const Epilogue &e, int64_t i0, int64_t j0) {
+__device__ inline void finish_blocks(const f32x4 (&acc)[kTI][kTJ], float *rows, const Product &a, const Epilogue &e, int64_t i0, int64_t j0, float *part, int ld) {
     constexpr int kRow = 16 * kTJ + 4, kUnits = 2 * kTJ, kTurns = 32 * kUnits / 64;
     const int lane = threadIdx.x % 64;
     const int col = lane % kUnits * 8;
     const int64_t j = j0 + col;
     const int valid = (int)std::min<int64_t>(8, a.nj - j);
     Columns<8> columns{};
-    if (!e.partial && valid > 0) columns = load_columns<O, 8>(j, valid, e);
+    if (!part && valid > 0) columns = load_columns<O, 8>(j, valid, e);
 #pragma unroll
     for (int x = 0; x < kTI; x += 2) {
 #pragma unroll
@@ -93,8 +94,8 @@ __device__ inline void finish_blocks(const f32x4 (&acc)[kTI][kTJ], float *rows, 
             if (i >= a.ni || valid <= 0) continue;
             const f32x4 lo = *(const f32x4 *)(rows + row * kRow + col), hi = *(const f32x4 *)(rows + row * kRow + col + 4);
             const vec<float, 8> z = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            if (e.partial) {
-                store_f32<float, 8>(e.partial + (blockIdx.y * a.ni + i) * a.nj + j, z, valid);
+            if (part) {
+                store_f32<float, 8>(part + (x * 16 + row) * ld + col, z, valid);
             } else {
                 vec<float, 8> residual(0.0f);
                 if (e.residual) residual = load_f32<O, 8>((const O *)e.residual + i * e.ldr + j, valid);
@@ -108,18 +109,19 @@ __device__ inline void finish_blocks(const f32x4 (&acc)[kTI][kTJ], float *rows, 
 // 16 kTI kDown x 16 kTJ kAcross of C by kDown x kAcross waves.
 template <typename O, bool kPowers, int kDown, int kAcross, int kTI, int kTJ>
 __global__ __launch_bounds__(64 * kDown * kAcross, 2) void product_blocks(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p,
-                                                                          int64_t r_bytes_q, int share_steps) {
+                                                                          int64_t r_bytes_q, int share_steps, int whole_tiles, int splits) {
     constexpr int kWaves = kDown * kAcross, kBI = 16 * kTI * kDown, kBJ = 16 * kTJ * kAcross;
     constexpr int kTileP = kBI * kStepBytes, kTileQ = kBJ * kStepBytes, kGroup = (kBI + 16) * 16;
     static_assert(kStepBytes == kScaled, "a step is a block of r");
     static_assert(kBJ / kScaled <= 16 && kScaled % (16 * kTJ) == 0, "a wave's columns share their scales");
     __shared__ __attribute__((aligned(1024))) char tiles[2 * kTileP + 2 * kTileQ + 2 * kGroup];
+    const TailBlock block = tail_block(blockIdx.x, whole_tiles, (int64_t)tiles_i * tiles_j, splits);
     int bi, bj;
-    tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
+    tile_of(block.tile, tiles_i, tiles_j, &bi, &bj);
     const int64_t i0 = (int64_t)bi * kBI, j0 = (int64_t)bj * kBJ;
     const int wave = wave_index(), lane = threadIdx.x % 64;
     const int wi = wave / kAcross * 16 * kTI, wj = wave % kAcross * 16 * kTJ;
-    const int64_t r0 = (int64_t)blockIdx.y * share_steps * kScaled, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kScaled);
+    const int64_t r0 = (int64_t)block.share * share_steps * kScaled, r1 = block.split ? std::min<int64_t>(a.nr, r0 + share_steps * kScaled) : a.nr;
     const int steps = (int)((r1 - r0 + kScaled - 1) / kScaled);
 
     Stream<e4m3, false, kBI, false, kWaves> sp;
@@ -201,7 +203,8 @@ __global__ __launch_bounds__(64 * kDown * kAcross, 2) void product_blocks(Produc
     }
     __syncthreads();
     static_assert(32 * (16 * kTJ + 4) * 4 * kWaves <= (int)sizeof(tiles), "the waves' shares fit the tiles' place");
-    finish_blocks<O, kTI, kTJ>(acc, (float *)&tiles[0] + wave * 32 * (16 * kTJ + 4), a, e, i0 + wi, j0 + wj);
+    finish_blocks<O, kTI, kTJ>(acc, (float *)&tiles[0] + wave * 32 * (16 * kTJ + 4), a, e, i0 + wi, j0 + wj,
+                               block.split ? e.partial + block.part * kBI * kBJ + wi * kBJ + wj : nullptr, kBJ);
 }
 
 // Rows of an operand on their way to a tile in LDS: kLoads times eight of them, from
@@ -247,16 +250,17 @@ struct RowStream {
 // and addresses only move from step to step.
 template <typename O, bool kPowers>
 __global__ __launch_bounds__(512, 2) void product_blocks_large(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p, int64_t r_bytes_q,
-                                                               int share_steps) {
+                                                               int share_steps, int whole_tiles, int splits) {
     constexpr int kB = 256, kTI = 8, kTJ = 4, kHalf = kTI / 2, kTile = kB * kStepBytes, kGroup = (kB + 16) * 16, kScalesAt = 4 * kTile;
     __shared__ __attribute__((aligned(1024))) char tiles[4 * kTile + 2 * kGroup];
+    const TailBlock block = tail_block(blockIdx.x, whole_tiles, (int64_t)tiles_i * tiles_j, splits);
     int bi, bj;
-    tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
+    tile_of(block.tile, tiles_i, tiles_j, &bi, &bj);
     const int64_t i0 = (int64_t)bi * kB, j0 = (int64_t)bj * kB;
     const int wave = wave_index(), lane = threadIdx.x % 64;
     const int wi = wave / 4 * 128, wj = wave % 4 * 64;
     const bool behind = wave >= 4;
-    const int64_t r0 = (int64_t)blockIdx.y * share_steps * kScaled, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kScaled);
+    const int64_t r0 = (int64_t)block.share * share_steps * kScaled, r1 = block.split ? std::min<int64_t>(a.nr, r0 + share_steps * kScaled) : a.nr;
     const int steps = (int)((r1 - r0 + kScaled - 1) / kScaled);
     f32x4 acc[kTI][kTJ] = {};
     if (steps > 0) {
@@ -405,7 +409,8 @@ __global__ __launch_bounds__(512, 2) void product_blocks_large(Product a, Epilog
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // the last loads, before this LDS has another use
     }
     __syncthreads();
-    finish_blocks<O, kTI, kTJ>(acc, (float *)&tiles[0] + wave * 32 * (16 * kTJ + 4), a, e, i0 + wi, j0 + wj);
+    finish_blocks<O, kTI, kTJ>(acc, (float *)&tiles[0] + wave * 32 * (16 * kTJ + 4), a, e, i0 + wi, j0 + wj,
+                               block.split ? e.partial + block.part * kB * kB + wi * kB + wj : nullptr, kB);
 }
 
 template <typename O, bool kPowers>
@@ -418,15 +423,15 @@ hipError_t launch_blocks(Product a, Epilogue e, char *ws, hipStream_t s) {
     const hipError_t r = pack_operands<e4m3, kForm, false, false>(a, p, r_bytes_p, ws, s);
     if (r != hipSuccess) return r;
     const int64_t r_bytes_q = p.pack_q ? a.ldq : a.nr;
-    const Cut &c = p.cut;
-    e.partial = c.splits > 1 ? (float *)(ws + p.p_bytes + p.q_bytes) : nullptr;
+    const TailCut &c = p.tail;
+    e.partial = (float *)(ws + p.p_bytes + p.q_bytes);
     const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, c.tile);
-    const dim3 grid(ti * tj, c.splits);
+    const dim3 grid((unsigned)(c.whole + c.tail * c.splits));
     if (c.tile == 256)
-        hipLaunchKernelGGL((product_blocks_large<O, kPowers>), grid, dim3(512), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
+        hipLaunchKernelGGL((product_blocks_large<O, kPowers>), grid, dim3(512), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share, c.whole, c.splits);
     else
-        hipLaunchKernelGGL((product_blocks<O, kPowers, 2, 2, 4, 4>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
-    return join<O, kOne>(a, e, c.splits, s);
+        hipLaunchKernelGGL((product_blocks<O, kPowers, 2, 2, 4, 4>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share, c.whole, c.splits);
+    return join_tail<O, kForm>(a, e, c, ti, tj, s);
 }
 
 Product product_of(const tg_block_linear_args &q) {

@@ -473,6 +473,19 @@ __device__ inline void tile_of(int64_t b, int ti, int tj, int *i, int *j) {
     *j = in / high;
 }
 
+// What block b of a tail cut does: its tile, its share of r, and where a share's sums
+// go, tile by tile.
+struct TailBlock {
+    int tile, share;
+    bool split;
+    int64_t part;  // of the sums, tiles of them
+};
+__device__ inline TailBlock tail_block(int64_t b, int64_t whole, int64_t tiles, int splits) {
+    if (b < whole || splits == 1) return {(int)b, 0, false, 0};
+    const int64_t x = b - whole, tail = tiles - whole;
+    return {(int)(whole + x % tail), (int)(x / tail), true, x % tail * splits + x / tail};
+}
+
 // f(kFrom), ..., f(kTo - 1) with the numbers known to the compiler.
 template <int kFrom, int kTo, typename F>
 __device__ inline void each(F f) {
@@ -490,7 +503,7 @@ constexpr int share(int n, int slots, int of) { return n >= slots ? of : (n * of
 // lane's sums are of gate and up for the same rows and columns.
 template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ, Form kForm = kOne>
 __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p,
-                                                                             int64_t r_bytes_q, int share_steps) {
+                                                                             int64_t r_bytes_q, int share_steps, int whole_tiles, int splits) {
     constexpr int kBI = 64 * kTI, kBJ = 64 * kTJ;
     constexpr bool kPair = kForm == kGated;
     constexpr int kDeep = Wide<T>::kDeep;
@@ -498,8 +511,11 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     constexpr int kTileP = kBI * kStepBytes, kTileQ = kBJ * kStepBytes;
     __shared__ __attribute__((aligned(1024))) char tiles[2 * kTileP + 3 * kTileQ];
     using frag = typename Wide<T>::frag;
+    // kOne: every tile in gridDim.y shares; else a tail cut
+    const TailBlock block = kForm == kOne ? TailBlock{(int)blockIdx.x, (int)blockIdx.y, true, 0}
+                                          : tail_block(blockIdx.x, whole_tiles, (int64_t)tiles_i * tiles_j, splits);
     int bi, bj;
-    tile_of(blockIdx.x, tiles_i, tiles_j, &bi, &bj);
+    tile_of(block.tile, tiles_i, tiles_j, &bi, &bj);
     const int64_t i0 = (int64_t)bi * kBI, j0 = (int64_t)bj * (kPair ? kBJ / 2 : kBJ);
     const int wave = wave_index(), lane = threadIdx.x % 64;
     const int wi = (wave / 2) * 32 * kTI, wj = (wave % 2) * (kPair ? 16 : 32) * kTJ;  // in C's tile
@@ -509,7 +525,7 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     Reader<T, kDownP, kBI> rp;
     Reader<T, kDownQ, kBJ, kPair ? kTJ / 2 : 64, 16 * kTJ> rq;
     // this block's share of r: all of it where there are no splits
-    const int64_t r0 = (int64_t)blockIdx.y * share_steps * kStep, r1 = std::min<int64_t>(a.nr, r0 + share_steps * kStep);
+    const int64_t r0 = (int64_t)block.share * share_steps * kStep, r1 = block.split ? std::min<int64_t>(a.nr, r0 + share_steps * kStep) : a.nr;
     sp.init(a.p, a.ldp, i0, a.ni, r0, r1, r1 < a.nr ? r1 * (int64_t)sizeof(T) : r_bytes_p);
     if constexpr (kForm == kSeam) {
         sq.init(a.q, a.ldq, j0, a.nj, r0, a.half, r_bytes_q);
@@ -631,6 +647,8 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     constexpr int kRow = 32 * kTJ + 4, kUnits = 2 * kTJ, kShare = 32 * kRow * 4 + 32 * 32 * kTJ * 2 + 128;
     static_assert(4 * kShare <= (int)sizeof(tiles), "the waves' shares fit the tiles' place");
     float *const rows = (float *)(&tiles[0] + wave * kShare);
+    // where a share's sums go, row by row of the tile
+    float *const part = kForm != kOne && block.split ? e.partial + block.part * kBI * kBJ : nullptr;
     if constexpr (kPair) {  // gate's 16 kTJ columns first in a row, then up's
         constexpr int kTurns = kTJ, kAcross = 2 * kTJ;
         float *const x_scales = rows + 32 * kRow;
@@ -638,7 +656,7 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
         const int64_t j = j0 + wj + col;
         const int valid = (int)std::min<int64_t>(8, a.nj - j);
         Columns<8> gates{}, ups{};
-        if (!e.partial && valid > 0) gates = load_columns<O, 8>(j, valid, e), ups = load_columns_up<O, 8>(j, valid, e);
+        if (!part && valid > 0) gates = load_columns<O, 8>(j, valid, e), ups = load_columns_up<O, 8>(j, valid, e);
 #pragma unroll
         for (int x = 0; x < kTI; ++x) {
 #pragma unroll
@@ -664,10 +682,10 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
                 const f32x4 u0 = *(const f32x4 *)(at + 16 * kTJ), u1 = *(const f32x4 *)(at + 16 * kTJ + 4);
                 const vec<float, 8> gate = __builtin_shufflevector(g0, g1, 0, 1, 2, 3, 4, 5, 6, 7);
                 const vec<float, 8> up = __builtin_shufflevector(u0, u1, 0, 1, 2, 3, 4, 5, 6, 7);
-                if (e.partial) {
-                    float *const to = e.partial + (blockIdx.y * a.ni + i) * (2 * a.nj) + j;
+                if (part) {
+                    float *const to = part + (i - i0) * kBJ + (j - j0);
                     store_f32<float, 8>(to, gate, valid);
-                    store_f32<float, 8>(to + a.nj, up, valid);
+                    store_f32<float, 8>(to + kBJ / 2, up, valid);
                 } else {
                     finish_gated<O, 8>(gate, up, e.x_scale ? x_scales[row] : 1.0f, gates, ups, i, j, valid, e);
                 }
@@ -696,7 +714,8 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
         const int64_t i = i0 + wi + x * 32 + lane % 32;
         if (e.x_scale) scale = i < a.ni ? e.x_scale[i] : 1.0f;
     };
-    if (!e.partial) {
+    const bool finished = kForm == kOne ? !e.partial : !part;
+    if (finished) {
         if (valid > 0) columns = load_columns<O, 8>(j, valid, e);
         fetch(0);
     }
@@ -710,7 +729,7 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
                 *(f32x4 *)(rows + (lane % 32) * kRow + y * 32 + 2 * c + (lane / 32) * 4) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
             }
         }
-        if (!e.partial) {
+        if (finished) {
             if (e.residual) {
 #pragma unroll
                 for (int n = 0; n < kUnits; ++n) kept[n * 64 + lane] = fetched[n];
@@ -726,9 +745,15 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
             const int row = (int)(i - i0 - wi) - x * 32;
             const f32x4 lo = *(const f32x4 *)(rows + row * kRow + col), hi = *(const f32x4 *)(rows + row * kRow + col + 4);
             const vec<float, 8> z = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            if (e.partial) {
+            if (kForm == kOne && e.partial) {
                 store_f32<float, 8>(e.partial + (blockIdx.y * a.ni + i) * a.nj + j, z, valid);
                 continue;
+            }
+            if constexpr (kForm != kOne) {
+                if (part) {
+                    store_f32<float, 8>(part + (i - i0) * kBJ + (j - j0), z, valid);
+                    continue;
+                }
             }
             if constexpr (kForm == kHalves) {
                 finish_halves<O, 8>(z, i, j, valid, e);
@@ -897,6 +922,42 @@ __global__ __launch_bounds__(256) void join_kernel(Epilogue e, int splits, int64
         finish<O, 8>(sum(j), i, j, valid, e);
 }
 
+// The same after a tail cut: 8 columns of a tile a thread, kTile^2 / 2048 blocks a
+// tile (of gated ones half as many).
+template <typename O, Form kForm, int kTile>
+__global__ __launch_bounds__(256) void join_tiles(Epilogue e, int whole, int splits, int tiles_i, int tiles_j, int64_t ni, int64_t nj) {
+    constexpr int kColumns = kForm == kGated ? kTile / 2 : kTile, kUnits = kColumns / 8, kPerTile = kTile * kUnits / 256;
+    const int tile = blockIdx.x / kPerTile, u = blockIdx.x % kPerTile * 256 + threadIdx.x, row = u / kUnits, col = u % kUnits * 8;
+    int bi, bj;
+    tile_of(whole + tile, tiles_i, tiles_j, &bi, &bj);
+    const int64_t i = (int64_t)bi * kTile + row, j = (int64_t)bj * kColumns + col;
+    if (i >= ni || j >= nj) return;
+    const int valid = (int)std::min<int64_t>(8, nj - j);
+    const float *const from = e.partial + (int64_t)tile * splits * kTile * kTile + row * kTile + col;
+    const auto sum = [&](int column) {
+        vec<float, 8> z = load_f32<float, 8>(from + column, 8);
+        for (int s = 1; s < splits; ++s) z += load_f32<float, 8>(from + column + (int64_t)s * kTile * kTile, 8);
+        return z;
+    };
+    if constexpr (kForm == kGated)
+        finish_gated<O, 8>(sum(0), sum(kTile / 2), i, j, valid, e);
+    else if constexpr (kForm == kHalves)
+        finish_halves<O, 8>(sum(0), i, j, valid, e);
+    else
+        finish<O, 8>(sum(0), i, j, valid, e);
+}
+template <typename O, Form kForm>
+hipError_t join_tail(const Product &a, const Epilogue &e, const TailCut &c, int ti, int tj, hipStream_t s) {
+    const hipError_t r = hipGetLastError();
+    if (r != hipSuccess || c.splits == 1) return r;
+    const dim3 grid((unsigned)(c.tail * (c.tile * c.tile / 2048) / (kForm == kGated ? 2 : 1)));
+    if (c.tile == 256)
+        hipLaunchKernelGGL((join_tiles<O, kForm, 256>), grid, dim3(256), 0, s, e, c.whole, c.splits, ti, tj, a.ni, a.nj);
+    else
+        hipLaunchKernelGGL((join_tiles<O, kForm, 128>), grid, dim3(256), 0, s, e, c.whole, c.splits, ti, tj, a.ni, a.nj);
+    return hipGetLastError();
+}
+
 constexpr int64_t kMostLd = 1 << 21;  // elements of a row of a product's operands
 
 inline size_t cut_bytes(const Cut &c, int64_t ni, int64_t nj) { return c.splits > 1 ? round256((size_t)c.splits * ni * nj * 4) : 0; }
@@ -941,7 +1002,8 @@ inline int64_t whole_ld(int64_t cols, int size) { return ceil_div(cols * size, 1
 // lies where in the workspace: packed P, packed Q (both of its matrices), shares.
 struct Plan {
     bool few, pack_p, pack_q;
-    Cut cut;
+    Cut cut;       // kOne, and `few`
+    TailCut tail;  // the other forms
     size_t p_bytes, q_bytes, bytes;
 };
 template <Form kForm = kOne>
@@ -971,11 +1033,14 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
         p.bytes = cut_bytes(p.cut, a.ni, columns);
         return p;
     }
-    p.cut = cut_product(a.ni, columns, a.nr, size);
+    if constexpr (kForm == kOne)
+        p.cut = cut_product(a.ni, columns, a.nr, size);
+    else
+        p.tail = cut_tail(a.ni, columns, a.nr, size);
     const auto packed = [&](int64_t n, int64_t r, bool down) { return round256(down ? r * whole_ld(n, size) * size : n * whole_ld(r, size) * size); };
     p.p_bytes = p.pack_p ? packed(a.ni, a.nr, down_p) : 0;
     p.q_bytes = p.pack_q ? packed(a.nj, kForm == kSeam ? a.half : a.nr, down_q) * (kTwo ? 2 : 1) : 0;
-    p.bytes = p.p_bytes + p.q_bytes + cut_bytes(p.cut, a.ni, columns);
+    p.bytes = p.p_bytes + p.q_bytes + (kForm == kOne ? cut_bytes(p.cut, a.ni, columns) : round256(p.tail.bytes()));
     return p;
 }
 
@@ -1040,15 +1105,26 @@ hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hi
     const hipError_t r = pack_operands<T, kForm, kDownP, kDownQ>(a, p, r_bytes_p, ws, s);
     if (r != hipSuccess) return r;
     const int64_t r_bytes_q = p.pack_q ? a.ldq * kSize : a.nr * kSize;
-    const Cut &c = p.cut;
-    e.partial = c.splits > 1 ? (float *)(ws + p.p_bytes + p.q_bytes) : nullptr;
-    const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, kForm == kGated ? c.tile / 2 : c.tile);
-    const dim3 grid(ti * tj, c.splits);
-    if (c.tile == 256)
-        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
-    else
-        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share);
-    return join<O, kForm>(a, e, c.splits, s);
+    float *const sums = (float *)(ws + p.p_bytes + p.q_bytes);
+    const auto go = [&](int tile, dim3 grid, int share, int whole, int splits) {
+        e.partial = splits > 1 ? sums : nullptr;
+        const int ti = (int)ceil_div(a.ni, tile), tj = (int)ceil_div(a.nj, kForm == kGated ? tile / 2 : tile);
+        if (tile == 256)
+            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, share, whole, splits);
+        else
+            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, share, whole, splits);
+        if constexpr (kForm == kOne)
+            return join<O, kForm>(a, e, splits, s);
+        else
+            return join_tail<O, kForm>(a, e, p.tail, ti, tj, s);
+    };
+    if constexpr (kForm == kOne) {
+        const Cut &c = p.cut;
+        return go(c.tile, dim3((unsigned)(ceil_div(a.ni, c.tile) * ceil_div(a.nj, c.tile)), c.splits), c.share, 0, c.splits);
+    } else {
+        const TailCut &c = p.tail;
+        return go(c.tile, dim3((unsigned)(c.whole + c.tail * c.splits)), c.share, c.whole, c.splits);
+    }
 }
 
 // ---------------------------------------------------------------------------
