@@ -26,6 +26,37 @@ struct GatedSlopeArgs {
     int act;
 };
 
+// act(z), and its slope, which share the exponential and the distribution function.
+// Beyond |z| = 128, where z may have been an infinity, as in slope(); the value is
+// z's own there, and NaN stays.
+template <int N>
+__device__ inline vec<float, N> value_and_slope(vec<float, N> z, int act, vec<float, N> *value) {
+    vec<float, N> s(1.0f);
+    *value = z;
+    if (act == TG_ACT_RELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            s[c] = z[c] > 0.0f ? 1.0f : 0.0f;
+            (*value)[c] = z[c] < 0.0f ? 0.0f : z[c];
+        }
+    } else if (act == TG_ACT_SILU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const float h = held(z[c]), t = __builtin_amdgcn_rcpf(1.0f + exp_f32(-h));
+            s[c] = t * fmaf(h, 1.0f - t, 1.0f);
+            (*value)[c] = z[c] * t;
+        }
+    } else if (act == TG_ACT_GELU) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const float h = held(z[c]), bell = exp_f32(-0.5f * h * h), cdf = normal_cdf(h, bell);
+            s[c] = fmaf(h * 0.39894228f, bell, cdf);
+            (*value)[c] = z[c] * cdf;
+        }
+    }
+    return s;
+}
+
 // 256 columns by 8 rows at a time; a block goes down its share of the rows.  dg and
 // du are rounded to the inputs' 16 bits because the matrix instructions of the
 // products read no more; the biases' sums take them before that.  Bound by memory:
@@ -44,9 +75,8 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(GatedSlopeArgs a) {
             const f32x8 dy = load_f32<E, 8>((const E *)a.dy + row * a.lddy + col, valid);
             const f32x8 gate = load_f32<E, 8>((const E *)a.gate + row * a.ldg + col, valid);
             const f32x8 up = load_f32<E, 8>((const E *)a.up + row * a.ldu + col, valid);
-            f32x8 d[2], value = gate;
-            d[0] = a.act == TG_ACT_NONE ? dy * up : dy * up * slope<8>(gate, a.act);
-            activate<8>(value, a.act);
+            f32x8 d[2], value;
+            d[0] = dy * up * value_and_slope<8>(gate, a.act, &value);
             d[1] = dy * value;
 #pragma unroll
             for (int o = 0; o < 2; ++o) {

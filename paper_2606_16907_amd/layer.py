@@ -25,6 +25,7 @@ do, and gradients are calls of their own.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -72,6 +73,19 @@ TgAdamwTensor = _struct("TgAdamwTensor", p=("param grad master m v m_scale v_sca
 TgAdamwRates = _struct("TgAdamwRates", r=("lr beta1 beta2 eps weight_decay grad_scale", ctypes.c_double),
                        n=("step", _i64), t=("seed reserved", ctypes.c_uint32))
 
+_CODES = {_vp: "Q", _i32: "i", _i64: "q", ctypes.c_float: "f"}
+
+
+def _packer(args):
+    """A function of the structure's fields, NULL as 0, to the bytes of the structure: a third of the time that ctypes
+    takes to fill one."""
+    return struct.Struct("@" + "".join(_CODES[t] for _, t in args._fields_)).pack
+
+
+_pack_gated, _pack_gated_grad, _pack_block_linear, _pack_quantize, _pack_layer_norm, _pack_layer_norm_grad = (
+    _packer(t) for t in (TgGatedArgs, TgGatedGradArgs, TgBlockLinearArgs, TgQuantizeArgs, TgLayerNormArgs,
+                         TgLayerNormGradArgs))
+
 EXPORTS = ("tg_linear_workspace_bytes", "tg_linear", "tg_linear_grad_workspace_bytes", "tg_linear_grad",
            "tg_gated_workspace_bytes", "tg_gated", "tg_gated_grad_workspace_bytes", "tg_gated_grad",
            "tg_block_linear_workspace_bytes", "tg_block_linear", "tg_quantize",
@@ -80,6 +94,7 @@ EXPORTS = ("tg_linear_workspace_bytes", "tg_linear", "tg_linear_grad_workspace_b
            "tg_adamw_create", "tg_adamw_step", "tg_adamw_destroy")
 
 _lib = None
+_bytes_calls = {}  # entry points that take their arguments as packed bytes
 
 
 def load_library():
@@ -102,6 +117,12 @@ def load_library():
     L.tg_adamw_create.argtypes = [P(TgAdamwTensor), _i32, _i32, _i32, _i32, P(_vp)]
     L.tg_adamw_step.argtypes = [_vp, P(TgAdamwRates), _vp]
     L.tg_adamw_destroy.argtypes, L.tg_adamw_destroy.restype = [_vp], None
+    for name in ("tg_gated", "tg_gated_grad", "tg_block_linear", "tg_quantize", "tg_layer_norm", "tg_layer_norm_grad"):
+        call = _bytes_calls[name] = L[name]  # an object of its own
+        call.argtypes = [ctypes.c_char_p] + getattr(L, name).argtypes[1:]
+        if hasattr(L, name + "_workspace_bytes"):
+            size = _bytes_calls[name + "_workspace_bytes"] = L[name + "_workspace_bytes"]
+            size.argtypes, size.restype = [ctypes.c_char_p], _sz
     _lib = L
     return L
 
@@ -153,6 +174,12 @@ def _workspace(size, given, like, device):
         return None, 0, None
     t = like.new_empty(size, dtype=torch.uint8)
     return t.data_ptr(), size, t
+
+
+def _call(name, args, given, like, device):
+    """Entry point `name` on packed arguments, with the workspace that it wants."""
+    ws, size, _kept = _workspace(_bytes_calls[name + "_workspace_bytes"](args), given, like, device)
+    T._check(_bytes_calls[name](args, ws, size, _stream(device)), name)
 
 
 def _act(act):
@@ -248,7 +275,7 @@ def tg_gated(x, w_gate, w_up, gate_bias=None, up_bias=None, act="silu", x_scale=
     (then x_scale [m], gate_scale [n] and up_scale [n] floats multiply the
     products, all or none, and the other operands have out_dtype, bfloat16 unless
     given).  Returns y, or with keep_pre (y, gate, up): what tg_gated_grad wants."""
-    lib = load_library()
+    load_library()
     device = torch.cuda.current_device()
     dtype = x.dtype
     if dtype not in TYPES or dtype == torch.float32:
@@ -265,18 +292,18 @@ def tg_gated(x, w_gate, w_up, gate_bias=None, up_bias=None, act="silu", x_scale=
     scales = (x_scale, gate_scale, up_scale)
     if any(s is not None for s in scales) and (dtype != E4M3 or any(s is None for s in scales)):
         raise ValueError("x_scale, gate_scale and up_scale come together, with 8-bit inputs")
-    psx, psg, psu = (None if s is None else _vector(s, torch.float32, size, what, device)
-                     for s, size, what in zip(scales, (m, n, n), ("x_scale", "gate_scale", "up_scale")))
-    pbg, pbu = (None if b is None else _vector(b, out_dtype, n, what, device)
-                for b, what in ((gate_bias, "gate_bias"), (up_bias, "up_bias")))
+    psx = 0 if x_scale is None else _vector(x_scale, torch.float32, m, "x_scale", device)
+    psg = 0 if gate_scale is None else _vector(gate_scale, torch.float32, n, "gate_scale", device)
+    psu = 0 if up_scale is None else _vector(up_scale, torch.float32, n, "up_scale", device)
+    pbg = 0 if gate_bias is None else _vector(gate_bias, out_dtype, n, "gate_bias", device)
+    pbu = 0 if up_bias is None else _vector(up_bias, out_dtype, n, "up_bias", device)
     act = _act(act)
     y, py, ldy = _out(out, x, m, n, out_dtype, device)
-    gate, pgate, ldg = _out(None, x, m, n, out_dtype, device) if keep_pre else (None, None, 0)
-    up, pup, ldu = _out(None, x, m, n, out_dtype, device) if keep_pre else (None, None, 0)
-    a = TgGatedArgs(px, pg, pu, psx, psg, psu, pbg, pbu, py, pgate, pup, m, n, k, ldx, ldwg, ldwu, ldy, ldg, ldu,
+    gate, pgate, ldg = _out(None, x, m, n, out_dtype, device) if keep_pre else (None, 0, 0)
+    up, pup, ldu = _out(None, x, m, n, out_dtype, device) if keep_pre else (None, 0, 0)
+    a = _pack_gated(px, pg, pu, psx, psg, psu, pbg, pbu, py, pgate, pup, m, n, k, ldx, ldwg, ldwu, ldy, ldg, ldu,
                     TYPES[dtype], TYPES[out_dtype], act, 0)
-    ws, size, _kept = _workspace(lib.tg_gated_workspace_bytes(a), workspace, x, device)
-    T._check(lib.tg_gated(a, ws, size, _stream(device)), "tg_gated")
+    _call("tg_gated", a, workspace, x, device)
     return (y, gate, up) if keep_pre else y
 
 
@@ -292,7 +319,7 @@ def tg_gated_grad(dy, x, w_gate, w_up, gate, up, act="silu", bias_grad=False, x_
                   dw_gate=None, dw_up=None, dgate_bias=None, dup_bias=None, workspace=None):
     """Gradients of tg_gated from dy [m, n], in the inputs' type; those not asked
     for are None, those given are written to.  `gate` and `up` are tg_gated's."""
-    lib = load_library()
+    load_library()
     device = torch.cuda.current_device()
     dtype = dy.dtype
     if dtype not in (torch.bfloat16, torch.float16):
@@ -306,15 +333,14 @@ def tg_gated_grad(dy, x, w_gate, w_up, gate, up, act="silu", bias_grad=False, x_
     pg, ldg = _matrix(gate, dtype, m, n, "gate", device)
     pu, ldu = _matrix(up, dtype, m, n, "up", device)
     act = _act(act)
-    dx, pdx, lddx = _out(dx, dy, m, k, dtype, device, "dx") if x_grad else (None, None, 0)
-    dwg, pdwg, lddwg = _out(dw_gate, dy, n, k, dtype, device, "dw_gate") if w_grad else (None, None, 0)
-    dwu, pdwu, lddwu = _out(dw_up, dy, n, k, dtype, device, "dw_up") if w_grad else (None, None, 0)
-    dbg, pdbg = _vector_out(dgate_bias, dy, n, device, "dgate_bias") if bias_grad else (None, None)
-    dbu, pdbu = _vector_out(dup_bias, dy, n, device, "dup_bias") if bias_grad else (None, None)
-    a = TgGatedGradArgs(pdy, pg, pu, px, pwg, pwu, pdx, pdwg, pdwu, pdbg, pdbu, m, n, k, lddy, ldg, ldu, ldx, ldwg, ldwu,
-                        lddx, lddwg, lddwu, TYPES[dtype], act)
-    ws, size, _kept = _workspace(lib.tg_gated_grad_workspace_bytes(a), workspace, dy, device)
-    T._check(lib.tg_gated_grad(a, ws, size, _stream(device)), "tg_gated_grad")
+    dx, pdx, lddx = _out(dx, dy, m, k, dtype, device, "dx") if x_grad else (None, 0, 0)
+    dwg, pdwg, lddwg = _out(dw_gate, dy, n, k, dtype, device, "dw_gate") if w_grad else (None, 0, 0)
+    dwu, pdwu, lddwu = _out(dw_up, dy, n, k, dtype, device, "dw_up") if w_grad else (None, 0, 0)
+    dbg, pdbg = _vector_out(dgate_bias, dy, n, device, "dgate_bias") if bias_grad else (None, 0)
+    dbu, pdbu = _vector_out(dup_bias, dy, n, device, "dup_bias") if bias_grad else (None, 0)
+    a = _pack_gated_grad(pdy, pg, pu, px, pwg, pwu, pdx, pdwg, pdwu, pdbg, pdbu, m, n, k, lddy, ldg, ldu, ldx, ldwg, ldwu,
+                         lddx, lddwg, lddwu, TYPES[dtype], act)
+    _call("tg_gated_grad", a, workspace, dy, device)
     return GatedGrads(dx, dwg, dwu, dbg, dbu)
 
 
@@ -328,7 +354,7 @@ def tg_quantize(x, block_rows=1, scale_dtype=torch.float32, out=None, scale=None
     consecutive columns of a row (block_rows 1) or of 128 rows (block_rows 128):
     max |x| / 448 over the block, or with scale_dtype float8_e8m0fnu the least
     power of two that is no smaller.  `out` and `scale` are written to where given."""
-    lib = load_library()
+    load_library()
     device = torch.cuda.current_device()
     dtype = x.dtype
     if dtype not in TYPES or dtype == E4M3:
@@ -341,8 +367,8 @@ def tg_quantize(x, block_rows=1, scale_dtype=torch.float32, out=None, scale=None
     rows, cols = x.shape
     y, py, ldy = _out(out, x, rows, cols, E4M3, device)
     scale, ps, lds = _out(scale, x, -(-rows // block_rows), -(-cols // BLOCK), scale_dtype, device, "scale")
-    a = TgQuantizeArgs(px, py, ps, rows, cols, ldx, ldy, lds, TYPES[dtype], SCALE_TYPES[scale_dtype], block_rows, 0)
-    T._check(lib.tg_quantize(a, _stream(device)), "tg_quantize")
+    a = _pack_quantize(px, py, ps, rows, cols, ldx, ldy, lds, TYPES[dtype], SCALE_TYPES[scale_dtype], block_rows, 0)
+    T._check(_bytes_calls["tg_quantize"](a, _stream(device)), "tg_quantize")
     return Quantized(y, scale)
 
 
@@ -353,7 +379,7 @@ def tg_block_linear(x, w, x_scale, w_scale, bias=None, act="none", residual=None
     every block of 128 x 128, w_scale [ceil(n / 128), ceil(k / 128)], both float32
     or both float8_e8m0fnu.  The other operands have out_dtype, bfloat16 or
     float16.  `out` receives y and may be the residual."""
-    lib = load_library()
+    load_library()
     device = torch.cuda.current_device()
     if x_scale.dtype not in SCALE_TYPES:
         raise ValueError(f"x_scale: dtype {x_scale.dtype}, float32 or float8_e8m0fnu expected")
@@ -365,13 +391,12 @@ def tg_block_linear(x, w, x_scale, w_scale, bias=None, act="none", residual=None
     n, blocks = w.shape[0], -(-k // BLOCK)
     pxs, ldxs = _matrix(x_scale, x_scale.dtype, m, blocks, "x_scale", device)
     pws, ldws = _matrix(w_scale, x_scale.dtype, -(-n // BLOCK), blocks, "w_scale", device)
-    pb = None if bias is None else _vector(bias, out_dtype, n, "bias", device)
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, out_dtype, m, n, "residual", device)
+    pb = 0 if bias is None else _vector(bias, out_dtype, n, "bias", device)
+    pr, ldr = (0, 0) if residual is None else _matrix(residual, out_dtype, m, n, "residual", device)
     y, py, ldy = _out(out, x, m, n, out_dtype, device)
-    a = TgBlockLinearArgs(px, pw, pxs, pws, pb, pr, py, m, n, k, ldx, ldw, ldxs, ldws, ldr, ldy,
-                          SCALE_TYPES[x_scale.dtype], TYPES[out_dtype], _act(act), 0)
-    ws, size, _kept = _workspace(lib.tg_block_linear_workspace_bytes(a), workspace, x, device)
-    T._check(lib.tg_block_linear(a, ws, size, _stream(device)), "tg_block_linear")
+    a = _pack_block_linear(px, pw, pxs, pws, pb, pr, py, m, n, k, ldx, ldw, ldxs, ldws, ldr, ldy,
+                           SCALE_TYPES[x_scale.dtype], TYPES[out_dtype], _act(act), 0)
+    _call("tg_block_linear", a, workspace, x, device)
     return y
 
 
@@ -450,7 +475,7 @@ def tg_layer_norm(x, weight, bias=None, residual=None, eps=1e-5, out_dtype=None,
     float8_e4m3fn y is y / scale for a scale per row.  mean and rstd, which the
     gradient takes, are returned with outputs in the inputs' type, or as keep_stats
     says."""
-    lib = load_library()
+    load_library()
     device = torch.cuda.current_device()
     dtype = x.dtype
     if dtype not in TYPES or dtype == E4M3:
@@ -462,17 +487,22 @@ def tg_layer_norm(x, weight, bias=None, residual=None, eps=1e-5, out_dtype=None,
     px, ldx = _matrix(x, dtype, None, None, "x", device)
     rows, cols = x.shape
     pw = _vector(weight, dtype, cols, "weight", device)
-    pb = None if bias is None else _vector(bias, dtype, cols, "bias", device)
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, dtype, rows, cols, "residual", device)
+    pb = 0 if bias is None else _vector(bias, dtype, cols, "bias", device)
+    pr, ldr = (0, 0) if residual is None else _matrix(residual, dtype, rows, cols, "residual", device)
     eight = out_dtype == E4M3
-    hidden, ph, ldh = (x, None, 0) if residual is None else _out(None, x, rows, cols, dtype, device)
+    hidden, ph, ldh = (x, 0, 0) if residual is None else _out(None, x, rows, cols, dtype, device)
     y, py, ldy = _out(out, x, rows, cols, out_dtype, device)
-    scale = x.new_empty(rows, dtype=torch.float32) if eight else None
-    keep = keep_stats or (keep_stats is None and not eight)
-    mean, rstd = (x.new_empty(rows, dtype=torch.float32) if keep else None for _ in range(2))
-    a = TgLayerNormArgs(px, pr, pw, pb, ph, py, *(None if t is None else t.data_ptr() for t in (scale, mean, rstd)), rows,
-                        cols, ldx, ldr, ldh, ldy, eps, TYPES[dtype], TYPES[out_dtype], 0)
-    T._check(lib.tg_layer_norm(a, _stream(device)), "tg_layer_norm")
+    scale = mean = rstd = None
+    ps = pm = pd = 0
+    if eight:
+        scale = x.new_empty(rows, dtype=torch.float32)
+        ps = scale.data_ptr()
+    if keep_stats or (keep_stats is None and not eight):
+        mean, rstd = x.new_empty(rows, dtype=torch.float32), x.new_empty(rows, dtype=torch.float32)
+        pm, pd = mean.data_ptr(), rstd.data_ptr()
+    a = _pack_layer_norm(px, pr, pw, pb, ph, py, ps, pm, pd, rows, cols, ldx, ldr, ldh, ldy, eps, TYPES[dtype],
+                         TYPES[out_dtype], 0)
+    T._check(_bytes_calls["tg_layer_norm"](a, _stream(device)), "tg_layer_norm")
     return LayerNorm(y, scale, hidden, mean, rstd)
 
 
@@ -482,7 +512,7 @@ def tg_layer_norm_grad(dy, hidden, weight, mean, rstd, dhidden=None, bias_grad=T
     dx is the gradient of x and of the residual alike.  dhidden is the gradient that
     arrives at `hidden` from further on; outputs are written to where they are given
     (dx may be dy or dhidden)."""
-    lib = load_library()
+    load_library()
     device = torch.cuda.current_device()
     dtype = dy.dtype
     if dtype not in TYPES or dtype == E4M3:
@@ -491,14 +521,13 @@ def tg_layer_norm_grad(dy, hidden, weight, mean, rstd, dhidden=None, bias_grad=T
     rows, cols = dy.shape
     ph, ldh = _matrix(hidden, dtype, rows, cols, "hidden", device)
     pw = _vector(weight, dtype, cols, "weight", device)
-    pm, ps = (_vector(t, torch.float32, rows, what, device) for t, what in ((mean, "mean"), (rstd, "rstd")))
-    pdh, lddh = (None, 0) if dhidden is None else _matrix(dhidden, dtype, rows, cols, "dhidden", device)
+    pm, ps = _vector(mean, torch.float32, rows, "mean", device), _vector(rstd, torch.float32, rows, "rstd", device)
+    pdh, lddh = (0, 0) if dhidden is None else _matrix(dhidden, dtype, rows, cols, "dhidden", device)
     dx, pdx, lddx = _out(dx, dy, rows, cols, dtype, device, "dx")
     dweight, pdw = _vector_out(dweight, dy, cols, device, "dweight")
-    dbias, pdb = _vector_out(dbias, dy, cols, device, "dbias") if bias_grad else (None, None)
-    a = TgLayerNormGradArgs(pdy, pdh, ph, pw, pm, ps, pdx, pdw, pdb, rows, cols, lddy, lddh, ldh, lddx, TYPES[dtype], 0)
-    ws, size, _kept = _workspace(lib.tg_layer_norm_grad_workspace_bytes(a), workspace, dy, device)
-    T._check(lib.tg_layer_norm_grad(a, ws, size, _stream(device)), "tg_layer_norm_grad")
+    dbias, pdb = _vector_out(dbias, dy, cols, device, "dbias") if bias_grad else (None, 0)
+    a = _pack_layer_norm_grad(pdy, pdh, ph, pw, pm, ps, pdx, pdw, pdb, rows, cols, lddy, lddh, ldh, lddx, TYPES[dtype], 0)
+    _call("tg_layer_norm_grad", a, workspace, dy, device)
     return dx, dweight, dbias
 
 
