@@ -21,7 +21,7 @@ namespace {
 struct GatedSlopeArgs {
     const void *dy, *gate, *up;
     void *dz;        // [m, 2 half]: dg and du, each padded with zeros to `half` columns; NULL: only the sums
-    float *partial;  // [2][gridDim.y, n] sums of dg's and du's rows, or NULL
+    float *partial;  // [2][rows, n] sums of dg's and du's rows, or NULL
     int64_t m, n, lddy, ldg, ldu, half;
     int act;
 };
@@ -60,9 +60,16 @@ __device__ inline vec<float, N> value_and_slope(vec<float, N> z, int act, vec<fl
 // 256 columns by 8 rows at a time; a block goes down its share of the rows.  dg and
 // du are rounded to the inputs' 16 bits because the matrix instructions of the
 // products read no more; the biases' sums take them before that.  Bound by memory:
-// three matrices read, two written.
+// three matrices read, two written.  Rows of blocks from `rows` on pack what the
+// products cannot stream.
 template <typename E>
-__global__ __launch_bounds__(256) void gated_slope_kernel(GatedSlopeArgs a) {
+__global__ __launch_bounds__(256) void gated_slope_kernel(GatedSlopeArgs a, Packing k, int rows) {
+    if ((int)blockIdx.y >= rows) {
+        const int64_t blocks = (int64_t)(gridDim.y - rows) * gridDim.x, block = (int64_t)(blockIdx.y - rows) * gridDim.x + blockIdx.x;
+#pragma unroll
+        for (int o = 0; o < 3; ++o) pack_body<E>(k, o, block, blocks);
+        return;
+    }
     using f32x8 = vec<float, 8>;
     __shared__ float strand[2][8][256 + 8];
     const int64_t col = (int64_t)blockIdx.x * 256 + (threadIdx.x % 32) * 8;
@@ -71,7 +78,7 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(GatedSlopeArgs a) {
     const int64_t width = a.dz ? a.half : a.n;
     f32x8 sum[2] = {f32x8(0.0f), f32x8(0.0f)};
     if (col < width) {
-        for (int64_t row = (int64_t)blockIdx.y * 8 + g; row < a.m; row += (int64_t)gridDim.y * 8) {
+        for (int64_t row = (int64_t)blockIdx.y * 8 + g; row < a.m; row += (int64_t)rows * 8) {
             const f32x8 dy = load_f32<E, 8>((const E *)a.dy + row * a.lddy + col, valid);
             const f32x8 gate = load_f32<E, 8>((const E *)a.gate + row * a.ldg + col, valid);
             const f32x8 up = load_f32<E, 8>((const E *)a.up + row * a.ldu + col, valid);
@@ -101,7 +108,7 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(GatedSlopeArgs a) {
         float total = strand[o][0][threadIdx.x];
 #pragma unroll
         for (int h = 1; h < 8; ++h) total += strand[o][h][threadIdx.x];
-        a.partial[((int64_t)o * gridDim.y + blockIdx.y) * a.n + out] = total;
+        a.partial[((int64_t)o * rows + blockIdx.y) * a.n + out] = total;
     }
 }
 
@@ -119,15 +126,58 @@ Product forward_product(const tg_gated_args &q) {
     return a;
 }
 
-// What tg_gated_grad does, and what lies where in its workspace: dg and du, sums,
-// and the place of the two products, which run one after the other.
+// Both gradients' products in one launch, in tiles of 128, a place on each CU for either: small ones leave half of
+// the GPU idle by themselves.
+struct OneOfTwo {
+    Product a;
+    Epilogue e;
+    int64_t r_bytes_p, r_bytes_q;
+    int tiles_i, tiles_j, share, whole, splits;
+    unsigned blocks, join_blocks;
+};
+template <Form kForm>
+OneOfTwo one_of_two(const Product &a, Epilogue e, int64_t r_bytes_p, int64_t r_bytes_q, const TailCut &c, float *sums) {
+    e.seam = a.seam, e.half = a.half, e.partial = sums;
+    return {a, e, r_bytes_p, r_bytes_q, (int)ceil_div(a.ni, 128), (int)ceil_div(a.nj, 128), c.share, c.whole, c.splits,
+            (unsigned)(c.whole + c.tail * c.splits), join_blocks<kForm>(c)};
+}
+template <typename E>
+__global__ __launch_bounds__(256, 2) void product_two(OneOfTwo dx, OneOfTwo dw) {
+    __shared__ __attribute__((aligned(1024))) char tiles[kPlace<2, 2>];
+    const auto run = [&](auto form, auto down_p, const OneOfTwo &p, int64_t b) {
+        const TailBlock block = tail_block(b, p.whole, (int64_t)p.tiles_i * p.tiles_j, p.splits);
+        product_body<E, E, down_p, true, 2, 2, form>(tiles, block, p.a, p.e, p.tiles_i, p.tiles_j, p.r_bytes_p, p.r_bytes_q, p.share);
+    };
+    if (blockIdx.x < dx.blocks)
+        run(std::integral_constant<Form, kSeam>{}, std::false_type{}, dx, blockIdx.x);
+    else
+        run(std::integral_constant<Form, kHalves>{}, std::true_type{}, dw, blockIdx.x - dx.blocks);
+}
+// What is left after them: the shares of both, and the biases' sums (32 columns of one bias a block).
+template <typename E>
+__global__ __launch_bounds__(256) void finish_two(OneOfTwo dx, OneOfTwo dw, const float *partial, int rows, int64_t n, E *bias, E *bias2) {
+    unsigned b = blockIdx.x;
+    if (b < dx.join_blocks) {
+        join_body<E, kSeam, 128>(b, dx.e, dx.whole, dx.splits, dx.tiles_i, dx.tiles_j, dx.a.ni, dx.a.nj);
+    } else if ((b -= dx.join_blocks) < dw.join_blocks) {
+        join_body<E, kHalves, 128>(b, dw.e, dw.whole, dw.splits, dw.tiles_i, dw.tiles_j, dw.a.ni, dw.a.nj);
+    } else {
+        b -= dw.join_blocks;
+        E *const out = b % 2 ? bias2 : bias;
+        if (out) column_sums_block(partial + (b % 2 ? rows * n : 0), rows, n, (int64_t)(b / 2) * 32, out);
+    }
+}
+
+// What tg_gated_grad does, and what lies where in its workspace: dg and du, the
+// biases' sums, packed weights, packed x, shares of dx and of the weights' gradients.
 struct GatedGradPlan {
-    bool dz, sums, weights;
+    bool dz, sums, weights, two, pack_w, pack_x;
     int64_t half;
     int rows;
-    size_t dz_bytes, sum_bytes, product_bytes;
+    size_t dz_bytes, sum_bytes, w_bytes, x_bytes, dx_bytes, dw_bytes;
     Product dx, dw;
-    size_t bytes() const { return dz_bytes + sum_bytes + product_bytes; }
+    TailCut cut_dx, cut_dw;
+    size_t bytes() const { return dz_bytes + sum_bytes + 2 * w_bytes + x_bytes + dx_bytes + dw_bytes; }
 };
 
 GatedGradPlan plan_grad(const tg_gated_grad_args &q, char *ws) {
@@ -146,36 +196,72 @@ GatedGradPlan plan_grad(const tg_gated_grad_args &q, char *ws) {
     const bool both = q.dw_gate && q.dw_up;
     p.dw = Product{ws + (both || q.dw_gate ? 0 : p.half * 2), q.x, ldz, ld_of(q.ldx, q.m, q.k, q.type), both ? ldz : p.half, q.k, q.m};
     p.dw.seam = p.half, p.dw.half = q.n;
-    if (q.dx) p.product_bytes = plan_product<kSeam>(p.dx, 2, ldz * 2, false, true).bytes;
-    if (p.weights) p.product_bytes = std::max(p.product_bytes, plan_product<kHalves>(p.dw, 2, 0, true, true).bytes);
+    if (q.m == 0 || q.n == 0 || q.k == 0) {  // empty sums or empty outputs: nothing is read
+        if (q.dx) p.cut_dx = cut_tail(p.dx.ni, p.dx.nj, 0, 2);
+        if (p.weights) p.cut_dw = cut_tail(p.dw.ni, p.dw.nj, 0, 2);
+        return p;
+    }
+    const int64_t packed_k = whole_ld(q.k, 2) * 2;
+    p.pack_w = q.dx && (!streams(p.dx.q, p.dx.ldq, 2, 0, true) || !streams(p.dx.q2, p.dx.ldq2, 2, 0, true) || p.dx.ldq != p.dx.ldq2);
+    p.pack_x = p.weights && !streams(p.dw.q, p.dw.ldq, 2, 0, true);
+    p.w_bytes = p.pack_w ? round256(q.n * packed_k) : 0;
+    p.x_bytes = p.pack_x ? round256(q.m * packed_k) : 0;
+    if (q.dx) p.cut_dx = cut_tail(p.dx.ni, p.dx.nj, p.dx.nr, 2);
+    if (p.weights) p.cut_dw = cut_tail(p.dw.ni, p.dw.nj, p.dw.nr, 2);
+    if (q.dx && p.weights) {
+        const TailCut dx = cut_tail(p.dx.ni, p.dx.nj, p.dx.nr, 2, true), dw = cut_tail(p.dw.ni, p.dw.nj, p.dw.nr, 2, true);
+        p.two = std::max(dx.us, dw.us) < p.cut_dx.us + p.cut_dw.us;
+        if (p.two) p.cut_dx = dx, p.cut_dw = dw;
+    }
+    p.dx_bytes = round256(p.cut_dx.bytes());
+    p.dw_bytes = round256(p.cut_dw.bytes());
+    if (!p.two && p.dx_bytes && p.dw_bytes) p.dx_bytes = std::max(p.dx_bytes, p.dw_bytes), p.dw_bytes = 0;  // one after the other
     return p;
 }
 
 template <typename E>
-tg_status run_grad(const tg_gated_grad_args &q, const GatedGradPlan &p, char *ws, hipStream_t s) {
-    char *const place = ws + p.dz_bytes + p.sum_bytes;
+tg_status run_grad(const tg_gated_grad_args &q, GatedGradPlan &p, char *ws, hipStream_t s) {
     float *const sums = (float *)(ws + p.dz_bytes);
+    char *const packed = ws + p.dz_bytes + p.sum_bytes;
+    float *const dx_sums = (float *)(packed + 2 * p.w_bytes + p.x_bytes);
+    float *const dw_sums = p.dw_bytes ? (float *)((char *)dx_sums + p.dx_bytes) : dx_sums;
+    Packing k{};
+    if (p.pack_w) {
+        pack_operand(k, 0, p.dx.q, p.dx.ldq, q.n, q.k, 2, packed);
+        pack_operand(k, 1, p.dx.q2, p.dx.ldq2, q.n, q.k, 2, packed + p.w_bytes);
+    }
+    if (p.pack_x) pack_operand(k, 2, p.dw.q, p.dw.ldq, q.m, q.k, 2, packed + 2 * p.w_bytes);
     if (q.m > 0 && q.n > 0) {
-        GatedSlopeArgs a{q.dy, q.gate, q.up, p.dz ? ws : nullptr, p.sums ? sums : nullptr, q.m, q.n, q.lddy, q.ldg, q.ldu, p.half, q.act};
-        hipLaunchKernelGGL(gated_slope_kernel<E>, dim3((unsigned)ceil_div(p.half, 256), p.rows), dim3(256), 0, s, a);
+        const GatedSlopeArgs a{q.dy, q.gate, q.up, p.dz ? ws : nullptr, p.sums ? sums : nullptr, q.m, q.n, q.lddy, q.ldg, q.ldu, p.half, q.act};
+        const int64_t across = ceil_div(p.half, 256);
+        const int64_t units = std::max({k.rows[0] * k.ld_to[0], k.rows[1] * k.ld_to[1], k.rows[2] * k.ld_to[2]}) / 8;
+        const unsigned more = (unsigned)ceil_div(std::min<int64_t>(2048, ceil_div(units, 256)), across);
+        hipLaunchKernelGGL(gated_slope_kernel<E>, dim3((unsigned)across, p.rows + more), dim3(256), 0, s, a, k, p.rows);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return device_failed(e, "gated_slope_kernel");
+    }
+    Epilogue ex{}, ew{};
+    ex.out = q.dx, ex.ldo = q.lddx;
+    ew.out = q.dw_gate ? q.dw_gate : q.dw_up, ew.ldo = q.dw_gate ? q.lddwg : q.lddwu;
+    ew.out2 = q.dw_up, ew.ldo2 = q.lddwu;
+    if (p.two) {
+        const OneOfTwo dx = one_of_two<kSeam>(p.dx, ex, p.dx.ldp * 2, 0, p.cut_dx, dx_sums), dw = one_of_two<kHalves>(p.dw, ew, 0, 0, p.cut_dw, dw_sums);
+        hipLaunchKernelGGL(product_two<E>, dim3(dx.blocks + dw.blocks), dim3(256), 0, s, dx, dw);
+        const unsigned rest = dx.join_blocks + dw.join_blocks + (p.sums ? 2 * (unsigned)ceil_div(q.n, 32) : 0);
+        if (rest) hipLaunchKernelGGL(finish_two<E>, dim3(rest), dim3(256), 0, s, dx, dw, sums, p.rows, q.n, (E *)q.dgate_bias, (E *)q.dup_bias);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? TG_OK : device_failed(e, "the gradients' products");
     }
     if (p.sums) {
         const hipError_t e = launch_column_sums_of_two(sums, q.m > 0 ? p.rows : 0, q.n, q.dgate_bias, q.dup_bias, q.type, s);
         if (e != hipSuccess) return device_failed(e, "column_sums");
     }
     if (q.dx) {
-        Epilogue e{};
-        e.out = q.dx, e.ldo = q.lddx;
-        const hipError_t r = launch_product<E, E, false, true, kSeam>(p.dx, e, p.dx.ldp * 2, place, s);
+        const hipError_t r = launch_tiles<E, E, false, true, kSeam>(p.dx, ex, p.dx.ldp * 2, 0, p.cut_dx, dx_sums, s);
         if (r != hipSuccess) return device_failed(r, "the product dg wg + du wu");
     }
     if (p.weights) {
-        Epilogue e{};
-        e.out = q.dw_gate ? q.dw_gate : q.dw_up, e.ldo = q.dw_gate ? q.lddwg : q.lddwu;
-        e.out2 = q.dw_up, e.ldo2 = q.lddwu;
-        const hipError_t r = launch_product<E, E, true, true, kHalves>(p.dw, e, 0, place, s);
+        const hipError_t r = launch_tiles<E, E, true, true, kHalves>(p.dw, ew, 0, 0, p.cut_dw, dw_sums, s);
         if (r != hipSuccess) return device_failed(r, "the products dg^T x and du^T x");
     }
     return TG_OK;
@@ -263,7 +349,7 @@ tg_status tg_gated_grad(const tg_gated_grad_args *q, void *d_ws, size_t ws_bytes
     }
     if (q->dgate_bias) TG_TRY(check_matrix(q->dgate_bias, 0, 1, q->n, q->type, "dgate_bias"));
     if (q->dup_bias) TG_TRY(check_matrix(q->dup_bias, 0, 1, q->n, q->type, "dup_bias"));
-    const GatedGradPlan p = plan_grad(*q, (char *)d_ws);
+    GatedGradPlan p = plan_grad(*q, (char *)d_ws);
     TG_TRY(check_workspace(d_ws, ws_bytes, p.bytes()));
     return q->type == TG_BF16 ? run_grad<bf16>(*q, p, (char *)d_ws, (hipStream_t)stream)
                               : run_grad<f16>(*q, p, (char *)d_ws, (hipStream_t)stream);

@@ -159,6 +159,28 @@ __device__ inline float block_reduce(float x, float *slots) {
     return x;
 }
 
+// One block's share of the sums over a table's rows: 32 columns from col0 on, by 256
+// threads.  Strand g of eight adds rows g, g + 8, ..., then the strands are added in
+// order: in place of float atomics, so that the result is the same every time.
+template <typename T>
+__device__ inline void column_sums_block(const float *__restrict__ partial, int rows, int64_t cols, int64_t col0, T *out) {
+    __shared__ float strand[8][33];
+    const int lane = threadIdx.x % 32, g = threadIdx.x / 32;
+    const int64_t col = col0 + lane;
+    float sum = 0.0f;
+    if (col < cols) {
+#pragma unroll 8
+        for (int r = g; r < rows; r += 8) sum += partial[r * cols + col];
+    }
+    strand[g][lane] = sum;
+    __syncthreads();
+    if (g == 0 && col < cols) {
+#pragma unroll
+        for (int h = 1; h < 8; ++h) sum += strand[h][lane];
+        out[col] = (T)sum;
+    }
+}
+
 // out[c] = the sum of partial[r][c] over rows r (reduce.hip: ascending r within
 // eight interleaved strands, then the strands in order).
 hipError_t launch_column_sums(const float *partial, int rows, int64_t cols, void *out, int type, hipStream_t s);

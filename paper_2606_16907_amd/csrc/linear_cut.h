@@ -54,18 +54,19 @@ inline Cut cut_product(int64_t ni, int64_t nj, int64_t nr, int size) {
 struct TailCut {
     int tile, whole, splits, share;  // share: steps of a split
     int64_t tail;                    // tiles that are split; 0 with splits 1
+    double us;                       // the estimate
     size_t bytes() const { return splits > 1 ? (size_t)tail * splits * tile * tile * 4 : 0; }
 };
-inline TailCut cut_tail(int64_t ni, int64_t nj, int64_t nr, int size) {
+// beside: in tiles of 128 with one place of each CU, where another product has the other.
+inline TailCut cut_tail(int64_t ni, int64_t nj, int64_t nr, int size, bool beside = false) {
     const int64_t steps = std::max<int64_t>(1, ceil_div(nr * size, kStepBytes));
-    TailCut best{256, 0, 1, (int)steps, 0};
-    double least = 0;
-    for (int tile = 256; tile >= 128; tile /= 2) {
-        const int64_t tiles = ceil_div(ni, tile) * ceil_div(nj, tile), places = tile == 256 ? 256 : 512;
+    TailCut best{};
+    for (int tile = beside ? 128 : 256; tile >= 128; tile /= 2) {
+        const int64_t tiles = ceil_div(ni, tile) * ceil_div(nj, tile), places = tile == 256 || beside ? 256 : 512;
         const auto time = [&](int64_t blocks, int64_t share) {
             if (blocks == 0) return 0.0;
             if (tile == 256) return ceil_div(blocks, 256) * (9 + share * (1.05 + 0.53 * std::min(1.0, blocks / 256.0)));
-            return blocks <= 256 ? 3 + share * (0.33 + 0.23 * blocks / 256.0) : ceil_div(blocks, 512) * (5 + share * 0.95);
+            return blocks <= 256 && !beside ? 3 + share * (0.33 + 0.23 * blocks / 256.0) : ceil_div(blocks, places) * (5 + share * 0.95);
         };
         for (int part = 0; part < 2; ++part) {
             const int64_t whole = part ? tiles / places * places : 0, tail = tiles - whole;
@@ -77,7 +78,7 @@ inline TailCut cut_tail(int64_t ni, int64_t nj, int64_t nr, int size) {
                 double us = time(whole, steps) + time(tail * splits, share);
                 const double moved = splits * (double)tail * tile * tile * 8;
                 if (splits > 1) us += 3 + moved / (moved < 64e6 ? 8e6 : 4e6);
-                if (least == 0 || us < least) least = us, best = TailCut{tile, (int)(splits > 1 ? whole : tiles), splits, share, splits > 1 ? tail : 0};
+                if (best.tile == 0 || us < best.us) best = TailCut{tile, (int)(splits > 1 ? whole : tiles), splits, share, splits > 1 ? tail : 0, us};
             }
         }
     }

@@ -497,23 +497,22 @@ __device__ inline void each(F f) {
 // How many of `of` things are to come before slot n, spread evenly over `slots`.
 constexpr int share(int n, int slots, int of) { return n >= slots ? of : (n * of + slots - 1) / slots; }
 
-// 64 kTI x 64 kTJ of C by four waves of 32 kTI x 32 kTJ.
+template <int kTI, int kTJ>
+constexpr int kPlace = (2 * 64 * kTI + 3 * 64 * kTJ) * kStepBytes;
+
+// 64 kTI x 64 kTJ of C by four waves of 32 kTI x 32 kTJ, in kPlace bytes of LDS.
 //   kGated: two of the waves bring rows of one matrix and two of the other, and each
 // wave multiplies half its share of Q's tile from one and half from the other, so a
 // lane's sums are of gate and up for the same rows and columns.
-template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ, Form kForm = kOne>
-__global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p,
-                                                                             int64_t r_bytes_q, int share_steps, int whole_tiles, int splits) {
+template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ, Form kForm>
+__device__ __forceinline__ void product_body(char *tiles, const TailBlock &block, const Product &a, const Epilogue &e, int tiles_i, int tiles_j,
+                                             int64_t r_bytes_p, int64_t r_bytes_q, int share_steps) {
     constexpr int kBI = 64 * kTI, kBJ = 64 * kTJ;
     constexpr bool kPair = kForm == kGated;
     constexpr int kDeep = Wide<T>::kDeep;
     constexpr int64_t kStep = kStepBytes / sizeof(T);
     constexpr int kTileP = kBI * kStepBytes, kTileQ = kBJ * kStepBytes;
-    __shared__ __attribute__((aligned(1024))) char tiles[2 * kTileP + 3 * kTileQ];
     using frag = typename Wide<T>::frag;
-    // kOne: every tile in gridDim.y shares; else a tail cut
-    const TailBlock block = kForm == kOne ? TailBlock{(int)blockIdx.x, (int)blockIdx.y, true, 0}
-                                          : tail_block(blockIdx.x, whole_tiles, (int64_t)tiles_i * tiles_j, splits);
     int bi, bj;
     tile_of(block.tile, tiles_i, tiles_j, &bi, &bj);
     const int64_t i0 = (int64_t)bi * kBI, j0 = (int64_t)bj * (kPair ? kBJ / 2 : kBJ);
@@ -645,7 +644,7 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
     // unrolled, so that the activations' code stays small.
     __syncthreads();
     constexpr int kRow = 32 * kTJ + 4, kUnits = 2 * kTJ, kShare = 32 * kRow * 4 + 32 * 32 * kTJ * 2 + 128;
-    static_assert(4 * kShare <= (int)sizeof(tiles), "the waves' shares fit the tiles' place");
+    static_assert(4 * kShare <= kPlace<kTI, kTJ>, "the waves' shares fit the tiles' place");
     float *const rows = (float *)(&tiles[0] + wave * kShare);
     // where a share's sums go, row by row of the tile
     float *const part = kForm != kOne && block.split ? e.partial + block.part * kBI * kBJ : nullptr;
@@ -765,6 +764,16 @@ __global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Pro
         }
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+template <typename T, typename O, bool kDownP, bool kDownQ, int kTI, int kTJ, Form kForm = kOne>
+__global__ __launch_bounds__(256, kTI * kTJ > 4 ? 1 : 2) void product_direct(Product a, Epilogue e, int tiles_i, int tiles_j, int64_t r_bytes_p,
+                                                                             int64_t r_bytes_q, int share_steps, int whole_tiles, int splits) {
+    __shared__ __attribute__((aligned(1024))) char tiles[kPlace<kTI, kTJ>];
+    // kOne: every tile in gridDim.y shares; else a tail cut
+    const TailBlock block = kForm == kOne ? TailBlock{(int)blockIdx.x, (int)blockIdx.y, true, 0}
+                                          : tail_block(blockIdx.x, whole_tiles, (int64_t)tiles_i * tiles_j, splits);
+    product_body<T, O, kDownP, kDownQ, kTI, kTJ, kForm>(tiles, block, a, e, tiles_i, tiles_j, r_bytes_p, r_bytes_q, share_steps);
 }
 
 // ---------------------------------------------------------------------------
@@ -925,9 +934,9 @@ __global__ __launch_bounds__(256) void join_kernel(Epilogue e, int splits, int64
 // The same after a tail cut: 8 columns of a tile a thread, kTile^2 / 2048 blocks a
 // tile (of gated ones half as many).
 template <typename O, Form kForm, int kTile>
-__global__ __launch_bounds__(256) void join_tiles(Epilogue e, int whole, int splits, int tiles_i, int tiles_j, int64_t ni, int64_t nj) {
+__device__ inline void join_body(int block, const Epilogue &e, int whole, int splits, int tiles_i, int tiles_j, int64_t ni, int64_t nj) {
     constexpr int kColumns = kForm == kGated ? kTile / 2 : kTile, kUnits = kColumns / 8, kPerTile = kTile * kUnits / 256;
-    const int tile = blockIdx.x / kPerTile, u = blockIdx.x % kPerTile * 256 + threadIdx.x, row = u / kUnits, col = u % kUnits * 8;
+    const int tile = block / kPerTile, u = block % kPerTile * 256 + threadIdx.x, row = u / kUnits, col = u % kUnits * 8;
     int bi, bj;
     tile_of(whole + tile, tiles_i, tiles_j, &bi, &bj);
     const int64_t i = (int64_t)bi * kTile + row, j = (int64_t)bj * kColumns + col;
@@ -946,11 +955,19 @@ __global__ __launch_bounds__(256) void join_tiles(Epilogue e, int whole, int spl
     else
         finish<O, 8>(sum(0), i, j, valid, e);
 }
+template <typename O, Form kForm, int kTile>
+__global__ __launch_bounds__(256) void join_tiles(Epilogue e, int whole, int splits, int tiles_i, int tiles_j, int64_t ni, int64_t nj) {
+    join_body<O, kForm, kTile>(blockIdx.x, e, whole, splits, tiles_i, tiles_j, ni, nj);
+}
+template <Form kForm>
+unsigned join_blocks(const TailCut &c) {
+    return c.splits == 1 ? 0 : (unsigned)(c.tail * (c.tile * c.tile / 2048) / (kForm == kGated ? 2 : 1));
+}
 template <typename O, Form kForm>
 hipError_t join_tail(const Product &a, const Epilogue &e, const TailCut &c, int ti, int tj, hipStream_t s) {
     const hipError_t r = hipGetLastError();
     if (r != hipSuccess || c.splits == 1) return r;
-    const dim3 grid((unsigned)(c.tail * (c.tile * c.tile / 2048) / (kForm == kGated ? 2 : 1)));
+    const dim3 grid(join_blocks<kForm>(c));
     if (c.tile == 256)
         hipLaunchKernelGGL((join_tiles<O, kForm, 256>), grid, dim3(256), 0, s, e, c.whole, c.splits, ti, tj, a.ni, a.nj);
     else
@@ -972,11 +989,10 @@ struct Packing {
     int64_t rows[3], cols[3], ld[3], ld_to[3];  // rows 0: none
 };
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(Packing a) {
+__device__ inline void pack_body(const Packing &a, int o, int64_t block, int64_t blocks) {
     constexpr int kN = 16 / sizeof(T);
-    const int o = blockIdx.y;
     const int64_t units = a.ld_to[o] / kN, all = a.rows[o] * units;
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < all; u += (int64_t)gridDim.x * 256) {
+    for (int64_t u = block * 256 + threadIdx.x; u < all; u += blocks * 256) {
         const int64_t row = u / units, col = u % units * kN;
         const T *const from = (const T *)a.from[o] + row * a.ld[o] + col;
         vec<T, kN> v;
@@ -988,6 +1004,18 @@ __global__ __launch_bounds__(256) void pack_kernel(Packing a) {
         }
         *(vec<T, kN> *)((T *)a.to[o] + row * a.ld_to[o] + col) = v;
     }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(Packing a) {
+    pack_body<T>(a, blockIdx.y, blockIdx.x, gridDim.x);
+}
+// Operand o of a packing: `cols` columns of each of `rows` rows, which are the packed ones from now on.
+inline void pack_operand(Packing &k, int o, const void *&from, int64_t &ld, int64_t rows, int64_t cols, int size, char *to) {
+    k.from[o] = from, k.to[o] = to, k.ld[o] = ld;
+    k.rows[o] = rows, k.cols[o] = cols;
+    k.ld_to[o] = ld = ceil_div(cols * size, 16) * 16 / size;
+    from = to;
 }
 
 // Whether operand rows start at 16-byte addresses, an operand with r along its
@@ -1062,10 +1090,7 @@ hipError_t pack_operands(Product &a, const Plan &p, int64_t &r_bytes_p, char *ws
     if (!(p.pack_p || p.pack_q) || a.nr == 0) return hipSuccess;
     Packing k{};
     const auto pack = [&](int o, const void *&from, int64_t &ld, int64_t n, int64_t r, bool down, char *to) {
-        k.from[o] = from, k.to[o] = to, k.ld[o] = ld;
-        k.rows[o] = down ? r : n, k.cols[o] = down ? n : r;
-        k.ld_to[o] = ld = whole_ld(k.cols[o], kSize);
-        from = to;
+        pack_operand(k, o, from, ld, down ? r : n, down ? n : r, kSize, to);
     };
     const int64_t r_q = kForm == kSeam ? a.half : a.nr;
     if (p.pack_p) pack(0, a.p, a.ldp, a.ni, a.nr, kDownP, ws), r_bytes_p = a.ldp * kSize;
@@ -1092,6 +1117,21 @@ hipError_t launch_few(const Product &a, Epilogue e, const Plan &p, char *ws, hip
     return join<O, kForm>(a, e, p.cut.splits, s);
 }
 
+// C in a tail cut's tiles, from operands that may be streamed; the cut's bytes are at `sums`.
+template <typename T, typename O, bool kDownP, bool kDownQ, Form kForm>
+hipError_t launch_tiles(const Product &a, Epilogue e, int64_t r_bytes_p, int64_t r_bytes_q, const TailCut &c, float *sums, hipStream_t s) {
+    if (a.ni == 0 || a.nj == 0) return hipSuccess;
+    e.seam = a.seam, e.half = a.half;
+    e.partial = sums;
+    const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, kForm == kGated ? c.tile / 2 : c.tile);
+    const dim3 grid((unsigned)(c.whole + c.tail * c.splits));
+    if (c.tile == 256)
+        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share, c.whole, c.splits);
+    else
+        hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share, c.whole, c.splits);
+    return join_tail<O, kForm>(a, e, c, ti, tj, s);
+}
+
 // C; `ws` holds the plan's bytes.
 template <typename T, typename O, bool kDownP, bool kDownQ, Form kForm = kOne>
 hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hipStream_t s) {
@@ -1106,24 +1146,17 @@ hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hi
     if (r != hipSuccess) return r;
     const int64_t r_bytes_q = p.pack_q ? a.ldq * kSize : a.nr * kSize;
     float *const sums = (float *)(ws + p.p_bytes + p.q_bytes);
-    const auto go = [&](int tile, dim3 grid, int share, int whole, int splits) {
-        e.partial = splits > 1 ? sums : nullptr;
-        const int ti = (int)ceil_div(a.ni, tile), tj = (int)ceil_div(a.nj, kForm == kGated ? tile / 2 : tile);
-        if (tile == 256)
-            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, share, whole, splits);
-        else
-            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2, kForm>), grid, dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, share, whole, splits);
-        if constexpr (kForm == kOne)
-            return join<O, kForm>(a, e, splits, s);
-        else
-            return join_tail<O, kForm>(a, e, p.tail, ti, tj, s);
-    };
     if constexpr (kForm == kOne) {
         const Cut &c = p.cut;
-        return go(c.tile, dim3((unsigned)(ceil_div(a.ni, c.tile) * ceil_div(a.nj, c.tile)), c.splits), c.share, 0, c.splits);
+        const int ti = (int)ceil_div(a.ni, c.tile), tj = (int)ceil_div(a.nj, c.tile);
+        e.partial = c.splits > 1 ? sums : nullptr;
+        if (c.tile == 256)
+            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 4, 4>), dim3(ti * tj, c.splits), dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share, 0, c.splits);
+        else
+            hipLaunchKernelGGL((product_direct<T, O, kDownP, kDownQ, 2, 2>), dim3(ti * tj, c.splits), dim3(256), 0, s, a, e, ti, tj, r_bytes_p, r_bytes_q, c.share, 0, c.splits);
+        return join<O, kForm>(a, e, c.splits, s);
     } else {
-        const TailCut &c = p.tail;
-        return go(c.tile, dim3((unsigned)(c.whole + c.tail * c.splits)), c.share, c.whole, c.splits);
+        return launch_tiles<T, O, kDownP, kDownQ, kForm>(a, e, r_bytes_p, r_bytes_q, p.tail, sums, s);
     }
 }
 

@@ -7,28 +7,11 @@
 namespace tg {
 namespace {
 
-// Adding up in place of float atomics keeps the order, and so the result, the
-// same every time.  A block has 32 columns by 8 strands; strand g adds rows
-// g, g + 8, ..., then the strands are added in order.
 // Row 1 of blocks, where there is one, does the second table.
 template <typename T>
 __global__ __launch_bounds__(256) void column_sums(const float *__restrict__ partial, int rows, int64_t cols, int64_t first, T *out, T *out2) {
     if (blockIdx.y) partial += rows * cols, out = out2;
-    __shared__ float strand[8][33];
-    const int lane = threadIdx.x % 32, g = threadIdx.x / 32;
-    const int64_t col = first + (int64_t)blockIdx.x * 32 + lane;
-    float sum = 0.0f;
-    if (col < cols) {
-#pragma unroll 8
-        for (int r = g; r < rows; r += 8) sum += partial[r * cols + col];
-    }
-    strand[g][lane] = sum;
-    __syncthreads();
-    if (g == 0 && col < cols) {
-#pragma unroll
-        for (int h = 1; h < 8; ++h) sum += strand[h][lane];
-        out[col] = (T)sum;
-    }
+    column_sums_block(partial, rows, cols, first + (int64_t)blockIdx.x * 32, out);
 }
 
 constexpr int64_t kMostColumns = 1 << 25;  // of a launch: a grid holds fewer than 2^32 threads, 8 a column and table
