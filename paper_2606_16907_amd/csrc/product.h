@@ -246,6 +246,27 @@ struct Unit {
         }
         return r;
     }
+    // The same for a row of `row` elements that ends there, valid being 0 or less past its
+    // end: read up to that end, with what lies before the unit, and shifted.
+    static __device__ raw load_last(const T *p, int64_t valid, int64_t row) {
+        if (row < 8) return load(p, valid);
+        const int cut = valid < 8 ? 8 - (int)valid : 0, bits = (cut < 8 ? cut : 0) * 8 * (int)sizeof(T);
+        raw r = reinterpret_cast<const Loose<raw, alignof(T)> *>(p - cut)->v;
+        uint64_t words[sizeof(T)];
+        __builtin_memcpy(words, &r, sizeof(r));
+        if constexpr (sizeof(T) == 1) {
+            words[0] >>= bits;
+        } else {
+            const uint64_t low = bits >= 64 ? words[1] : words[0], high = bits >= 64 ? 0 : words[1];
+            const int rest = bits % 64;
+            words[0] = low >> rest | (high << 1) << (63 - rest);
+            words[1] = high >> rest;
+        }
+#pragma unroll
+        for (int w = 0; w < (int)sizeof(T); ++w) words[w] = cut < 8 ? words[w] : 0;
+        __builtin_memcpy(&r, words, sizeof(r));
+        return r;
+    }
 };
 __device__ inline i32x4 widened(i32x4 u) { return u; }
 // e4m3 values are bf16 values too.
@@ -859,16 +880,43 @@ __global__ __launch_bounds__(512) void product_few(Product a, Epilogue e, int64_
             for (int u = 0; u < kUnits; ++u) ux[m][u] = Unit<T>::load(x[m] + turn * kTurn + at(u), 8);
         multiply(turn, uw, ux);
     }
-    if (whole * kTurn < a.nr && blockIdx.y + 1 == gridDim.y && wave == (whole - begin) % kWaves) {
-        raw uw[kUnits], ux[kRows][kUnits];
+    const bool last = whole * kTurn < a.nr && blockIdx.y + 1 == gridDim.y;  // the turn that the row's end cuts
+    if constexpr (kForm == kOne) {
+        if (last && wave == (whole - begin) % kWaves) {
+            raw uw[kUnits], ux[kRows][kUnits];
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u) {
-            const int64_t r = whole * kTurn + at(u);
-            uw[u] = Unit<T>::load(w + r, a.nr - r);
+            for (int u = 0; u < kUnits; ++u) {
+                const int64_t r = whole * kTurn + at(u);
+                uw[u] = Unit<T>::load(w + r, a.nr - r);
 #pragma unroll
-            for (int m = 0; m < kRows; ++m) ux[m][u] = Unit<T>::load(x[m] + r, a.nr - r);
+                for (int m = 0; m < kRows; ++m) ux[m][u] = Unit<T>::load(x[m] + r, a.nr - r);
+            }
+            multiply(whole, uw, ux);
         }
-        multiply(whole, uw, ux);
+    } else if (last) {  // its units in turn among the waves: 1040 e4m3 elements, one row through 26558, take 15 us, by one wave 31
+#pragma unroll
+        for (int n = 0; n < kUnits / kWaves; ++n) {
+            const int u = wave + n * kWaves;
+            const int64_t r = whole * kTurn + at(u);
+            if (whole * kTurn + at(u) - at(0) >= a.nr) continue;
+            const raw uw = Unit<T>::load_last(w + r, a.nr - r, a.nr);
+            raw ux[kRows];
+#pragma unroll
+            for (int m = 0; m < kRows; ++m) ux[m] = Unit<T>::load_last(x[m] + r, a.nr - r, a.nr);
+            const frag fw = __builtin_bit_cast(frag, widened(uw));
+#pragma unroll
+            for (int m = 0; m < kRows; ++m) {
+                if constexpr (kScales) {
+                    const int64_t b = whole * 4 + u / 4;
+                    const f32x4 part = Matrix<C>::mma(fw, __builtin_bit_cast(frag, widened(ux[m])), f32x4(0.0f));
+                    const float s = load_scales<kForm == kExponents>(x_scales[m], b, b + 1)[0] * load_scales<kForm == kExponents>(w_scales, b, b + 1)[0];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[m][c] = fmaf(part[c], s, acc[m][c]);
+                } else {
+                    acc[m] = Matrix<C>::mma(fw, __builtin_bit_cast(frag, widened(ux[m])), acc[m]);
+                }
+            }
+        }
     }
 #pragma unroll
     for (int m = 0; m < kRows; ++m) sums[wave][m][lane] = acc[m];
