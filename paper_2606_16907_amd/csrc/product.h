@@ -1094,7 +1094,11 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
     // From some 8 rows on tiles of 128 and splits are as fast: 4096 x 14336 in
     // bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at 16.
     // Where an operand would have to be packed, up to 64 rows.
-    p.few = !down_p && !down_q && a.ni <= (p.pack_p || p.pack_q ? 64 : 8);
+    int64_t most_few = p.pack_p || p.pack_q ? 64 : 8;
+    // In the newer forms up to where packing w is cheaper: with W million bytes of it
+    // product_few takes 4 + W (0.25 + 0.021 rows) us, packing and tiles 12 + 0.47 W.
+    if (kForm != kOne && most_few > 8) most_few = std::min<int64_t>(64, 10 + 380000000 / std::max<int64_t>(1, columns * a.nr * size));
+    p.few = !down_p && !down_q && a.ni <= most_few;
     if (p.few) {
         // Few rows of w leave most of the chip idle: sums of 40 turns and more are
         // shared out among blocks then, a turn a wave at least.  4 rows through 689 x
