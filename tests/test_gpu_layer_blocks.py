@@ -157,7 +157,7 @@ def test_block_linear(m, k, n, powers, pad):
 
 
 @pytest.mark.parametrize("powers", [False, True])
-@pytest.mark.parametrize("m,k,n,pad", [(1, 14336, 1024, 0), (4, 20483, 33, 5), (1500, 8200, 3000, 8), (3500, 2064, 4075, 0), (3841, 1999, 3841, 3), (3000, 16400, 1500, 0)])
+@pytest.mark.parametrize("m,k,n,pad", [(1, 14336, 1024, 0), (4, 20483, 33, 5), (1500, 8200, 3000, 8), (3500, 2064, 4075, 0), (3841, 1999, 3841, 3), (3000, 16400, 1500, 0), (4352, 4100, 4352, 0)])
 def test_shared_sums_and_large_tiles(m, k, n, pad, powers):
     check(m, k, n, powers, pad, residual=True)
 

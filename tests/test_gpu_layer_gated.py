@@ -62,7 +62,8 @@ def test_forward_in_8_bits(m, k, n, pad, out):
 
 
 @pytest.mark.parametrize("m,k,n,pad,dtype", [(1, 8192, 9, 0, BF16), (1, 14336, 640, 0, BF16), (4, 10803, 345, 3, F16), (8, 14336, 512, 0, BF16),
-                                             (600, 6000, 300, 0, F16), (1500, 8200, 1500, 0, BF16), (3500, 1000, 2041, 8, BF16)])
+                                             (600, 6000, 300, 0, F16), (1500, 8200, 1500, 0, BF16), (3500, 1000, 2041, 8, BF16),
+                                             (4352, 2056, 2176, 0, BF16), (4200, 1000, 4100, 3, F16)])
 def test_shared_sums_and_large_tiles(m, k, n, pad, dtype):
     gen = R.generator("gated large", m, k, n, pad)
     x, wg, wu = R.rows(gen, m, k, dtype, pad), R.rows(gen, n, k, dtype, pad, k ** -0.5), R.rows(gen, n, k, dtype, 0, k ** -0.5)
@@ -88,7 +89,7 @@ def test_gradients(m, k, n, dtype, pad):
         R.within(getattr(got, key), *want, key)
 
 
-@pytest.mark.parametrize("m,k,n", [(300, 3400, 8200), (8200, 1500, 700), (2048, 520, 2050)])
+@pytest.mark.parametrize("m,k,n", [(300, 3400, 8200), (8200, 1500, 700), (2048, 520, 2050), (4352, 4352, 1024)])
 def test_gradients_of_large_tiles_and_shared_sums(m, k, n):
     gen = R.generator("gated large grad", m, k, n)
     x, wg, wu = R.rows(gen, m, k, BF16), R.rows(gen, n, k, BF16, 0, k ** -0.5), R.rows(gen, n, k, BF16, 0, k ** -0.5)
