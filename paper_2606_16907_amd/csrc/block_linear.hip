@@ -347,13 +347,12 @@ __global__ __launch_bounds__(512, 2) void product_blocks_large(Product a, Epilog
             const char *const from = &tiles[0] + x_scale + scales;
 #pragma unroll
             for (int x = 0; x < kHalf; ++x) s[x] = *(const word *)(from + (half * kHalf + x) * 256);
-        };
-        const auto multiply = [&](auto half) {
-            __builtin_amdgcn_s_setprio(1);
             if constexpr (!kPowers) {
 #pragma unroll
                 for (int x = 0; x < kHalf; ++x) s[x] *= sw;
             }
+        };
+        const auto multiply = [&](auto half) {
             each<0, kHalf * kTJ>([&](auto n) {
                 constexpr int x = n / kTJ, y = n % kTJ;
                 if constexpr (kPowers) {
@@ -367,7 +366,6 @@ __global__ __launch_bounds__(512, 2) void product_blocks_large(Product a, Epilog
             });
             if constexpr (kPowers)
                 each<0, kHalf * kTJ>([&](auto n) { settled(acc[half * kHalf + n / kTJ][n % kTJ]); });
-            __builtin_amdgcn_s_setprio(0);
         };
         // what multiply leaves over runs beside the other wave's matrix instructions
         const auto rest = [&](auto half) {

@@ -27,12 +27,13 @@ __device__ inline vec<float, kUnitOf<E>> floats(i32x4 bits) {
 // The compiler does not know from here on what the bits became before.
 __device__ inline void forget(i32x4 &bits) { asm volatile("" : "+v"(bits)); }
 
-// dx, and a row of sums for dweight and dbias from each block.  T threads have a row;
+// dx, and a row of sums for dweight and dbias from each block; one block alone writes
+// dweight and dbias themselves.  T threads have a row;
 // with T = 64 a block has kRows of them at a time, else one.  A row stays in 16-byte
 // units as it was read, converted in both passes over it, so that there is room for
 // the next row, on its way meanwhile (kAhead); the sums of a thread's columns stay in registers over all rows.
 template <typename E, int T, int N, int kRows, bool kAhead>
-__global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a) {
+__global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a, E *dweight, E *dbias) {  // NULL: sums to a.partial
     constexpr int kUnit = kUnitOf<E>;
     using unit = vec<float, kUnit>;
     static_assert(T == 64 || kRows == 1, "rows that meet at barriers have a block of their own");
@@ -125,23 +126,39 @@ __global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a) {
     for (int n = 0; n < N; ++n) {
         const int64_t at = (int64_t)blockIdx.x * a.cols + (t + n * T) * kUnit;
         if (valid(n) <= 0) continue;
+        if (dweight) {
+            store_f32<E, kUnit>(dweight + at, dw[n], valid(n));
+            if (dbias) store_f32<E, kUnit>(dbias + at, db[n], valid(n));
+            continue;
+        }
         store_f32<float, kUnit>(a.partial + at, dw[n], valid(n));
         if (a.partial2) store_f32<float, kUnit>(a.partial2 + at, db[n], valid(n));
     }
 }
 
-// Blocks of the gradient: each leaves a row of sums for the weight and one for the
-// bias.
+int64_t units_of(int64_t cols, int type) { return ceil_div(cols * (type == TG_F32 ? 4 : 2), 16); }
+constexpr int64_t kMostUnits = 2048;  // of a row that stays in registers
+
+// Few rows are left to one block, which writes the gradients itself and takes less than
+// the launch that adds up several (eight waves with a row each; 2 us a row of many).
+bool one_block(int64_t rows, int64_t cols, int type) {
+    const int64_t units = units_of(cols, type);
+    return rows > 0 && (units <= 128 ? rows <= 64 : units <= kMostUnits && rows <= 2);
+}
+
+// Blocks of the gradient: but for a single one, each leaves a row of sums for the weight
+// and one for the bias.
 int layer_grad_blocks(int64_t rows, int64_t cols, int type) {
-    const int64_t units = ceil_div(cols * (type == TG_F32 ? 4 : 2), 16);
+    const int64_t units = units_of(cols, type);
+    if (one_block(rows, cols, type)) return 1;
     const int64_t most = units <= 128 ? ceil_div(rows, 8) : rows;
-    return (int)std::min<int64_t>(most, units <= 1024 || units > 2048 ? 512 : 256);
+    return (int)std::min<int64_t>(most, units <= 1024 || units > kMostUnits ? 512 : 256);
 }
 
 template <typename E>
-hipError_t launch_layer_grad(GradArgs a, int blocks, hipStream_t s) {
+hipError_t launch_layer_grad(GradArgs a, int blocks, void *dweight, void *dbias, hipStream_t s) {
     const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
-    const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, s, a); };
+    const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, s, a, (E *)dweight, (E *)dbias); };
     if (units <= 64)
         go(layer_norm_grad_kernel<E, 64, 1, 8, true>, 512);
     else if (units <= 128)
@@ -154,7 +171,7 @@ hipError_t launch_layer_grad(GradArgs a, int blocks, hipStream_t s) {
         go(layer_norm_grad_kernel<E, 512, 2, 1, true>, 512);
     else if (units <= 1536)
         go(layer_norm_grad_kernel<E, 768, 2, 1, true>, 768);
-    else if (units <= 2048)
+    else if (units <= kMostUnits)
         go(layer_norm_grad_kernel<E, 1024, 2, 1, false>, 1024);
     else
         launch_grad_stream<E, true>(a, blocks, s);
@@ -206,6 +223,7 @@ tg_status tg_layer_norm(const tg_layer_norm_args *q, tg_stream stream) {
 
 size_t tg_layer_norm_grad_workspace_bytes(const tg_layer_norm_grad_args *q) {
     if (!q || q->rows < 0 || q->cols < 0 || q->rows > 0x7fffffff || q->cols > 0x7fffffff - 64) return 0;
+    if (one_block(q->rows, q->cols, q->type)) return 0;
     return round256((size_t)layer_grad_blocks(q->rows, q->cols, q->type) * q->cols * (q->dbias ? 8 : 4));
 }
 
@@ -229,18 +247,21 @@ tg_status tg_layer_norm_grad(const tg_layer_norm_grad_args *q, void *d_ws, size_
         if (q->dhidden) TG_TRY(check_rows(q->dhidden, q->lddh, q->rows, q->cols, q->type, "dhidden"));
         if ((uintptr_t)d_ws % 256) return call_failed(TG_EINVAL, "the workspace is not 256-byte aligned");
         const size_t need = tg_layer_norm_grad_workspace_bytes(q);
-        if (ws_bytes < need || !d_ws) return call_failed(TG_ENOMEM, "workspace of %zu bytes, %zu needed", d_ws ? ws_bytes : 0, need);
+        if (need && (ws_bytes < need || !d_ws)) return call_failed(TG_ENOMEM, "workspace of %zu bytes, %zu needed", d_ws ? ws_bytes : 0, need);
         const bool one = q->rows == 1;
         float *const sums = (float *)d_ws;
         const int blocks = layer_grad_blocks(q->rows, q->cols, q->type);
+        const bool alone = one_block(q->rows, q->cols, q->type);
+        void *const dweight = alone ? q->dweight : nullptr, *const dbias = alone ? q->dbias : nullptr;
         GradArgs a{q->dy, q->dhidden, q->hidden, q->weight, q->mean, q->rstd, q->dx, sums,
                    q->dbias ? sums + (int64_t)blocks * q->cols : nullptr, q->rows,
                    one ? 0 : q->lddy, one ? 0 : q->lddh, one ? 0 : q->ldh, one ? 0 : q->lddx,
                    0, (int)q->cols, (float)(1.0 / (double)q->cols)};
-        e = q->type == TG_F32    ? launch_layer_grad<float>(a, blocks, s)
-            : q->type == TG_BF16 ? launch_layer_grad<bf16>(a, blocks, s)
-                                 : launch_layer_grad<f16>(a, blocks, s);
+        e = q->type == TG_F32    ? launch_layer_grad<float>(a, blocks, dweight, dbias, s)
+            : q->type == TG_BF16 ? launch_layer_grad<bf16>(a, blocks, dweight, dbias, s)
+                                 : launch_layer_grad<f16>(a, blocks, dweight, dbias, s);
         if (e != hipSuccess) return device_failed(e, "norm_grad_kernel");
+        if (alone) return TG_OK;
     }
     e = launch_column_sums_of_two((const float *)d_ws, layer_grad_blocks(q->rows, q->cols, q->type), q->cols, q->dweight, q->dbias, q->type, s);
     return e == hipSuccess ? TG_OK : device_failed(e, "column_sums");

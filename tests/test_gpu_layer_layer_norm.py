@@ -87,7 +87,7 @@ def test_forward_in_8_bits(rows, cols, dtype):
     assert float(f.y.float().abs().max()) <= 448.0
 
 
-@pytest.mark.parametrize("rows,cols", SHAPES + [(0, 40), (700, 72), (1030, 513), (1100, 40)])
+@pytest.mark.parametrize("rows,cols", SHAPES + [(0, 40), (700, 72), (1030, 513), (1100, 40), (64, 500), (65, 500), (1, 33000), (0, 33000), (2, 5000)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("pad", [0, 5])
 def test_gradients(rows, cols, dtype, pad):
