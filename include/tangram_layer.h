@@ -34,8 +34,7 @@
  *     bits, and results are rounded once, to nearest even.  (Products of 8-bit
  *     elements in large sizes are added in groups of eight by the matrix
  *     instruction, which cuts each off at 2^-13 of the power of two in a
- *     group's largest;
- *     those of a few rows of x are exact.)
+ *     group's largest; those of a few rows of x are exact.)
  *     Results are repeatable bit for bit on one device.
  *   - NaN and infinities propagate as the formulas say.
  *   - Errors: TG_EINVAL for an invalid argument, TG_ENOMEM for a workspace
@@ -144,7 +143,8 @@ tg_status tg_gated(const tg_gated_args *a, void *d_ws, size_t ws_bytes, tg_strea
 /*
  * Gradients of tg_gated for 16-bit types, from dy [m, n] and what it kept:
  *   dgate = dy up act'(gate), dup = dy act(gate), each rounded once to `type`, the
- *        type that the matrix instructions read (act' as in tg_linear_grad);
+ *        type that the matrix instructions read (where `gate` is an infinity, act'
+ *        and act have their limits there);
  *   dx [m, k] = dgate w_gate + dup w_up, dw_gate [n, k] = dgate^T x, dw_up [n, k] =
  *        dup^T x, dgate_bias and dup_bias [n] = the sums of dgate's and dup's rows
  *        (before those are rounded).
@@ -169,8 +169,9 @@ tg_status tg_gated_grad(const tg_gated_grad_args *a, void *d_ws, size_t ws_bytes
  *             scale_type, TG_F32 or TG_E8M0; matrices with row strides ldxs, ldws
  *   out_type  of bias, residual and y: TG_BF16 or TG_F16
  *   bias      [n] or NULL; residual [m, n] or NULL, may be y itself
- * A block's sum is added to the others in 32 bits after it is scaled.  Sizes as in
- * tg_linear.
+ * A block's sum is added to the others in 32 bits after it is scaled, by the product
+ * of its two scales, which has to be within the range of 32 bits.  Sizes as in
+ * tg_linear; row strides of scales below 2^21.
  */
 typedef struct {
     const void *x, *w, *x_scale, *w_scale;
@@ -258,7 +259,7 @@ tg_status tg_rms_norm_grad(const tg_rms_norm_grad_args *a, void *d_ws, size_t ws
  *   bias        [cols] or NULL, of `type`
  *   mean        [rows] floats or NULL
  * The deviations' squares are added after the mean is taken off; rows whose
- * deviations pass 1.8e19 have rstd 0.
+ * deviations pass 1.8e19 have rstd 0, those whose sum passes 3.4e38 become NaN.
  */
 typedef struct {
     const void *x, *residual, *weight, *bias;

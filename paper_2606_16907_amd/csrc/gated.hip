@@ -31,8 +31,8 @@ struct GatedSlopeArgs {
 };
 
 // act(z), and its slope, which share the exponential and the distribution function.
-// Beyond |z| = 128, where z may have been an infinity, as in slope(); the value is
-// z's own there, and NaN stays.
+// z comes in 16 bits, where one that was finite may be an infinity: beyond |z| = 128
+// the slope is its limit as in slope(), and so is the value, 0 below and z above.
 template <int N>
 __device__ inline vec<float, N> value_and_slope(vec<float, N> z, int act, vec<float, N> *value) {
     vec<float, N> s(1.0f);
@@ -48,14 +48,14 @@ __device__ inline vec<float, N> value_and_slope(vec<float, N> z, int act, vec<fl
         for (int c = 0; c < N; ++c) {
             const float h = held(z[c]), t = __builtin_amdgcn_rcpf(1.0f + exp_f32(-h));
             s[c] = t * fmaf(h, 1.0f - t, 1.0f);
-            (*value)[c] = z[c] * t;
+            (*value)[c] = (z[c] > 128.0f ? z[c] : h) * t;
         }
     } else if (act == TG_ACT_GELU) {
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             const float h = held(z[c]), bell = exp_f32(-0.5f * h * h), cdf = normal_cdf(h, bell);
             s[c] = fmaf(h * 0.39894228f, bell, cdf);
-            (*value)[c] = z[c] * cdf;
+            (*value)[c] = (z[c] > 128.0f ? z[c] : h) * cdf;
         }
     }
     return s;
@@ -217,6 +217,8 @@ GatedGradPlan plan_grad(const tg_gated_grad_args &q, char *ws) {
     if (q.dx && p.weights) {
         const TailCut dx = cut_tail(p.dx.ni, p.dx.nj, p.dx.nr, 2, true), dw = cut_tail(p.dw.ni, p.dw.nj, p.dw.nr, 2, true);
         p.two = std::max(dx.us, dw.us) < p.cut_dx.us + p.cut_dw.us;
+        // a grid holds fewer than 2^32 threads, 256 a block
+        p.two = p.two && dx.whole + dx.tail * dx.splits + dw.whole + dw.tail * dw.splits < (1 << 24);
         if (p.two) p.cut_dx = dx, p.cut_dw = dw;
     }
     p.dx_bytes = round256(p.cut_dx.bytes());

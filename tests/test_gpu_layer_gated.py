@@ -219,8 +219,34 @@ def test_pre_activations_that_are_infinities():
     x, w = torch.ones(1, 8, device="cuda", dtype=BF16), torch.eye(2, 8, device="cuda", dtype=BF16)
     gate = torch.tensor([[float("-inf"), float("inf")]], device="cuda", dtype=BF16)
     up, dy = torch.ones(1, 2, device="cuda", dtype=BF16), torch.ones(1, 2, device="cuda", dtype=BF16)
-    g = L.tg_gated_grad(dy, x, w, w, gate, up, act="silu", bias_grad=True)
-    assert g.dgate_bias.tolist() == [0.0, 1.0]
+    for name in ("silu", "gelu", "relu"):
+        g = L.tg_gated_grad(dy, x, w, w, gate, up, act=name, bias_grad=True)
+        assert g.dgate_bias.tolist() == [0.0, 1.0] and g.dup_bias.tolist() == [0.0, float("inf")], name
+
+
+def test_gradients_of_large_pre_activations():
+    """Where exp(-z) or exp(-z^2 / 2) leave 32 bits the slopes and values are 0 below, 1 and z above."""
+    L, gen = layer(), R.generator("large gates")
+    z = torch.tensor([-3e4, -1000.0, -200.0, -128.5, -127.0, -89.0, -20.0, 20.0, 89.0, 128.5, 1000.0, 3e4])
+    m, n, k = 5, len(z), 24
+    gate, up, dy = z.repeat(m, 1).to(F16).cuda(), R.rows(gen, m, n, F16), R.rows(gen, m, n, F16, std=2.0 ** -8)
+    x, wg, wu = R.rows(gen, m, k, F16), R.rows(gen, n, k, F16), R.rows(gen, n, k, F16)
+    for name in ACTS:
+        got = L.tg_gated_grad(dy, x, wg, wu, gate, up, act=name, bias_grad=True)
+        for key, want in G.grads(dy, x, wg, wu, gate, up, name).items():
+            R.within(getattr(got, key), *want, f"{name} {key}")
+
+
+def test_8_bits_without_scales_and_kept():
+    L, gen = layer(), R.generator("no scales")
+    for m in (3, 150):
+        x, wg, wu = (R.rows(gen, r, 200, torch.float32).to(E4M3) for r in (m, 90, 90))
+        y, gate, up = L.tg_gated(x, wg, wu, act="gelu", keep_pre=True)
+        one = [torch.ones(r, device="cuda") for r in (m, 90, 90)]
+        want = G.projections(x, wg, wu, None, None, *one)
+        R.within(gate, *G.kept(*want[0], BF16), "gate")
+        R.within(up, *G.kept(*want[1], BF16), "up")
+        R.within(y, *G.forward(*want, "gelu", BF16), "y")
 
 
 def test_halves_of_one_weight_and_outputs_that_are_given():

@@ -209,6 +209,21 @@ def test_outputs_in_the_place_of_inputs(rows, cols):
         assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
+@pytest.mark.parametrize("rows,cols", [(70, 1000), (3, 40000), (300, 12288)])
+@pytest.mark.parametrize("place", ["x", "residual"])
+def test_hidden_in_the_place_of_an_input(rows, cols, place):
+    """Through the C entry, which allows it."""
+    import ctypes
+    L, gen = layer(), R.generator("ln hidden", rows, cols)
+    x, r, w = R.rows(gen, rows, cols, BF16), R.rows(gen, rows, cols, BF16), R.rows(gen, 1, cols, BF16)[0]
+    want = L.tg_layer_norm(x, w, residual=r)
+    y, hidden = torch.empty_like(x), x if place == "x" else r
+    a = L.TgLayerNormArgs(x.data_ptr(), r.data_ptr(), w.data_ptr(), None, hidden.data_ptr(), y.data_ptr(), None, None, None, rows, cols, cols, cols, cols,
+                          cols, EPS, 1, 1, 0)
+    assert L.load_library().tg_layer_norm(ctypes.byref(a), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(y, want.y) and torch.equal(hidden, want.hidden)
+
+
 def test_repeatable_and_replayed():
     L = layer()
     gen = R.generator("ln graph")
