@@ -1095,8 +1095,8 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
     // bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at 16.
     // Where an operand would have to be packed, up to 64 rows.
     int64_t most_few = p.pack_p || p.pack_q ? 64 : 8;
-    // In the newer forms up to where packing w is cheaper: with W million bytes of it
-    // product_few takes 4 + W (0.25 + 0.021 rows) us, packing and tiles 12 + 0.47 W.
+    // With two weights or scaled blocks up to where packing w is cheaper: with W
+    // million bytes of it product_few takes 4 + W (0.25 + 0.021 rows) us, packing and tiles 12 + 0.47 W.
     if (kForm != kOne && most_few > 8) most_few = std::min<int64_t>(64, 10 + 380000000 / std::max<int64_t>(1, columns * a.nr * size));
     p.few = !down_p && !down_q && a.ni <= most_few;
     if (p.few) {
