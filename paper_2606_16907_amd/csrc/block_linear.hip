@@ -466,7 +466,8 @@ extern "C" {
 
 size_t tg_block_linear_workspace_bytes(const tg_block_linear_args *q) {
     if (!q || !sizes_fit(q->m, q->n, q->k)) return 0;
-    return plan_product<kBlocks>(product_of(*q), 1, q->k, false, false).bytes;
+    const Product a = product_of(*q);
+    return (q->scale_type == TG_F32 ? plan_product<kBlocks>(a, 1, q->k, false, false) : plan_product<kExponents>(a, 1, q->k, false, false)).bytes;
 }
 
 tg_status tg_block_linear(const tg_block_linear_args *q, void *d_ws, size_t ws_bytes, tg_stream stream) {
