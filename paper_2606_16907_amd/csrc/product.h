@@ -1095,6 +1095,20 @@ struct Plan {
 // floats, where 16 bits take 0.58.
 template <Form kForm>
 constexpr double pace_of(int size) { return kForm == kBlocks ? 1.4 : kForm == kExponents ? 1.25 : size == 1 ? 1.1 : 1.0; }
+// Rows of x up to which product_few is faster than tiles, with two weights or scaled
+// blocks.  Up to 16 it reads as much: 16 rows through 7168 x 4096 take 12.6 us with
+// scaled blocks and 11.5 gated in 8 bits, in tiles 17.5 and 17.2; through 4096 x 14336
+// 23 and 21 in tiles 23 and 19; from 100 MB on 12 rows (16384 x 16384: 75 for 75, 16
+// rows 84 for 76).  Up to 8192 columns tiles are few and split, which is another
+// launch: 32 rows through 7168 x 4096 take 15.8 for 17.9, through 4096 x 4096 10.3 for
+// 16.8, 64 rows through 2048 x 2048 9.8 for 19.2; longer rows read x again at every
+// block (64 through 7168 x 2048: 20.3 for 19.4).
+inline int64_t few_rows(int64_t columns, int64_t row_bytes) {
+    const int64_t all = columns * row_bytes;
+    if (columns <= 8192 && row_bytes <= 4096 && all <= 17000000) return 64;
+    if (columns <= 8192 && row_bytes <= 8192 && all <= 30000000) return 32;
+    return all <= 100000000 ? 16 : 12;
+}
 template <Form kForm = kOne>
 Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bool down_q) {
     Plan p{};
@@ -1104,13 +1118,14 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
     p.pack_p = !streams(a.p, a.ldp, size, r_bytes_p, down_p);
     p.pack_q = !streams(a.q, a.ldq, size, a.nr * size, down_q) || (kTwo && !streams(a.q2, a.ldq2, size, a.nr * size, down_q)) ||
                (kForm == kSeam && a.ldq != a.ldq2);
-    // From some 8 rows on tiles of 128 and splits are as fast: 4096 x 14336 in
+    // From some 8 rows on tiles of 128 and splits are as fast with one weight: 4096 x 14336 in
     // bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at 16.
     // Where an operand would have to be packed, up to 64 rows.
     int64_t most_few = p.pack_p || p.pack_q ? 64 : 8;
     // With two weights or scaled blocks up to where packing w is cheaper: with W
     // million bytes of it product_few takes 4 + W (0.25 + 0.021 rows) us, packing and tiles 12 + 0.47 W.
-    if (kForm != kOne && most_few > 8) most_few = std::min<int64_t>(64, 10 + 380000000 / std::max<int64_t>(1, columns * a.nr * size));
+    const int64_t row = a.nr * size, all = columns * row;  // bytes of w
+    if (kForm != kOne) most_few = most_few > 8 ? std::min<int64_t>(64, 10 + 380000000 / std::max<int64_t>(1, all)) : few_rows(columns, row);
     p.few = !down_p && !down_q && a.ni <= most_few;
     if (p.few) {
         // Few rows of w leave most of the chip idle: sums of 40 turns and more are

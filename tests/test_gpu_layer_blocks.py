@@ -151,7 +151,7 @@ def check(m, k, n, powers, pad, act="none", bias=False, residual=False, out=BF16
 @pytest.mark.parametrize("powers", [False, True])
 @pytest.mark.parametrize("pad", [0, 3, 16])
 @pytest.mark.parametrize("m,k,n", [(1, 1, 1), (1, 128, 16), (1, 4096, 130), (3, 129, 17), (8, 640, 257), (9, 256, 128), (16, 1000, 129), (33, 127, 300),
-                                   (64, 2048, 100), (65, 513, 129), (128, 128, 128), (130, 1152, 255), (257, 300, 520), (300, 4096, 136), (600, 1040, 1030)])
+                                   (64, 2048, 100), (17, 4096, 8300), (40, 8200, 520), (65, 513, 129), (128, 128, 128), (130, 1152, 255), (257, 300, 520), (300, 4096, 136), (600, 1040, 1030)])
 def test_block_linear(m, k, n, powers, pad):
     check(m, k, n, powers, pad, act=["none", "relu", "silu", "gelu"][(m + n) % 4], bias=bool(k % 2), residual=bool(m % 2), out=[BF16, F16][n % 2])
 

@@ -63,7 +63,7 @@ def test_forward_in_8_bits(m, k, n, pad, out):
 
 @pytest.mark.parametrize("m,k,n,pad,dtype", [(1, 8192, 9, 0, BF16), (1, 14336, 640, 0, BF16), (4, 10803, 345, 3, F16), (8, 14336, 512, 0, BF16),
                                              (600, 6000, 300, 0, F16), (1500, 8200, 1500, 0, BF16), (3500, 1000, 2041, 8, BF16),
-                                             (4352, 2056, 2176, 0, BF16), (4200, 1000, 4100, 3, F16), (4352, 4104, 2176, 0, BF16)])
+                                             (16, 4096, 5000, 0, BF16), (24, 2048, 4500, 0, F16), (50, 4100, 1030, 2, BF16), (4352, 2056, 2176, 0, BF16), (4200, 1000, 4100, 3, F16), (4352, 4104, 2176, 0, BF16)])
 def test_shared_sums_and_large_tiles(m, k, n, pad, dtype):
     gen = R.generator("gated large", m, k, n, pad)
     x, wg, wu = R.rows(gen, m, k, dtype, pad), R.rows(gen, n, k, dtype, pad, k ** -0.5), R.rows(gen, n, k, dtype, 0, k ** -0.5)
