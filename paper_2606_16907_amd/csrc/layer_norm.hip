@@ -24,6 +24,27 @@ __device__ inline i32x4 load_bits(const E *p, int valid) {
     }
     return r;
 }
+// The same of a row's unit at `col` in one load: of a last unit that is not whole the
+// row's last 16 bytes, for in_place to move down when they are used.  (With a load and
+// a branch for each element of it 16384 x 1605 in bf16 took 119 us, so 64.)
+template <typename E>
+__device__ inline i32x4 load_unit(const E *row, int col, int valid) {
+    constexpr int kUnit = kUnitOf<E>;
+    if (valid <= 0) return i32x4(0);
+    if (col == 0 && valid < kUnit) return load_bits<E>(row, valid);
+    return ((const Global<Loose<i32x4, alignof(E)>> *)(row + col + std::min(valid, kUnit) - kUnit))->v;
+}
+template <typename E>
+__device__ inline void in_place(i32x4 &r, int col, int valid) {
+    if (valid <= 0 || valid >= kUnitOf<E> || col == 0) return;
+    const int bits = (kUnitOf<E> - valid) * (int)sizeof(E) * 8;
+    if (bits & 64) r = i32x4{r[2], r[3], 0, 0};
+    if (bits & 32) r = i32x4{r[1], r[2], r[3], 0};
+    if (sizeof(E) == 2 && (bits & 16)) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r[w] = (int)((unsigned)r[w] >> 16 | (w < 3 ? (unsigned)r[w + 1] << 16 : 0));
+    }
+}
 template <typename E>
 __device__ inline vec<float, kUnitOf<E>> floats(i32x4 bits) {
     return __builtin_convertvector(__builtin_bit_cast(vec<E, kUnitOf<E>>, bits), vec<float, kUnitOf<E>>);
@@ -32,13 +53,15 @@ __device__ inline vec<float, kUnitOf<E>> floats(i32x4 bits) {
 __device__ inline void forget(i32x4 &bits) { asm volatile("" : "+v"(bits)); }
 
 // dx, and a row of sums for dweight and dbias from each block; one block alone writes
-// dweight and dbias themselves.  T threads have a row;
-// with T = 64 a block has kRows of them at a time, else one.  A row stays in 16-byte
-// units as it was read, converted in both passes over it, so that there is room for
-// the next row, on its way meanwhile (kAhead); the sums of a thread's columns stay in registers over all rows.
+// dweight and dbias themselves.  T threads have a row; with T = 64 a block has kRows of
+// them at a time, else one.  A row stays in 16-byte units as it was read, converted in
+// both passes over it, so that there is room for the next row, on its way meanwhile
+// (kAhead); the sums of a thread's columns stay in registers over all rows.
 template <typename E, int T, int N, int kRows, bool kAhead>
 __global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a, E *dweight, E *dbias) {  // NULL: sums to a.partial
     constexpr int kUnit = kUnitOf<E>;
+    // 768 threads have no registers left for it: 3001 x 12289 in f16 takes 90 us, so 104
+    constexpr bool kOneLoad = T < 768;
     using unit = vec<float, kUnit>;
     static_assert(T == 64 || kRows == 1, "rows that meet at barriers have a block of their own");
     __shared__ unit sums[2][T == 64 ? N * 64 : 1];
@@ -62,9 +85,10 @@ __global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a, E
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int col = (t + n * T) * kUnit, left = valid(n);
-            r.g[n] = load_bits<E>(dy + col, left);
-            r.h[n] = load_bits<E>(hidden + col, left);
-            r.more[n] = dh ? load_bits<E>(dh + col, left) : i32x4(0);
+            const auto load = [&](const E *p) { return kOneLoad ? load_unit<E>(p, col, left) : load_bits<E>(p + col, left); };
+            r.g[n] = load(dy);
+            r.h[n] = load(hidden);
+            r.more[n] = dh ? load(dh) : i32x4(0);
         }
         r.mean = a.mean[row], r.rstd = a.rstd[row];
     };
@@ -81,6 +105,8 @@ __global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a, E
         Two two{0.0f, 0.0f};
 #pragma unroll
         for (int n = 0; n < N; ++n) {
+            const int col = (t + n * T) * kUnit, left = valid(n);
+            if constexpr (kOneLoad) in_place<E>(now.g[n], col, left), in_place<E>(now.h[n], col, left), in_place<E>(now.more[n], col, left);
             const unit g = floats<E>(now.g[n]), h = floats<E>(now.h[n]), w = floats<E>(weight[n]);
 #pragma unroll
             for (int e = 0; e < kUnit; ++e) {
@@ -143,6 +169,10 @@ __global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a, E
 int64_t units_of(int64_t cols, int type) { return ceil_div(cols * (type == TG_F32 ? 4 : 2), 16); }
 constexpr int64_t kMostUnits = 2048;  // of a row that stays in registers
 
+// A wave has a row, eight of them a block, where its units leave room in registers for
+// the next row's: three a lane, of floats four.
+bool wave_has_a_row(int64_t units, int type) { return units <= (type == TG_F32 ? 256 : 192); }
+
 // Few rows are left to one block, which writes the gradients itself and takes less than
 // the launch that adds up several (eight waves with a row each; 2 us a row of many).
 bool one_block(int64_t rows, int64_t cols, int type) {
@@ -158,25 +188,31 @@ bool one_block(int64_t rows, int64_t cols, int type) {
 int layer_grad_blocks(int64_t rows, int64_t cols, int type) {
     const int64_t units = units_of(cols, type);
     if (one_block(rows, cols, type)) return 1;
-    const int64_t most = units <= 128 ? ceil_div(rows, 8) : rows;
-    return (int)std::min<int64_t>(most, units <= 128 ? 256 : units <= 256 ? 768 : units <= 512 || units > kMostUnits ? 512 : 256);
+    const bool waves = wave_has_a_row(units, type);
+    return (int)std::min<int64_t>(waves ? ceil_div(rows, 8) : rows, waves ? 256 : units <= 256 ? 768 : units <= 512 || units > kMostUnits ? 512 : 256);
 }
 
 template <typename E>
 hipError_t launch_layer_grad(GradArgs a, int blocks, void *dweight, void *dbias, hipStream_t s) {
     const int units = (a.cols + kUnitOf<E> - 1) / kUnitOf<E>;
     const auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, s, a, (E *)dweight, (E *)dbias); };
-    // A wave has a row while that is at most two units a lane, eight of them a block:
-    // 16384 x 512 in bf16 18 us, where blocks of one wave took 47.  Longer
-    // rows get threads for two units, in steps of 256, so that few have none: 8192 x
-    // 12288 takes 162 us by 768 threads and 213 by 1024 (without the row ahead).
+    // 16384 x 512 in bf16 takes 18 us, where blocks of one wave took 47; 16384 x 1304 42
+    // and 50 by 256 threads a row, 16384 x 2048 58 and 103 by a wave, whose registers do
+    // not hold four units and the next; 16384 x 520 of floats 33 and 40.  Longer rows
+    // get threads for two units, in steps of 256, so that few have none: 8192 x 12288
+    // takes 162 us by 768 threads and 213 by 1024 (without the row ahead).
     if (units <= 64)
         go(layer_norm_grad_kernel<E, 64, 1, 8, true>, 512);
     else if (units <= 128)
         go(layer_norm_grad_kernel<E, 64, 2, 8, true>, 512);
-    else if (units <= 256)
-        go(layer_norm_grad_kernel<E, 256, 1, 1, true>, 256);
-    else if (units <= 512)
+    else if (units <= 192)
+        go(layer_norm_grad_kernel<E, 64, 3, 8, true>, 512);
+    else if (units <= 256) {
+        if constexpr (sizeof(E) == 4)
+            go(layer_norm_grad_kernel<E, 64, 4, 8, true>, 512);
+        else
+            go(layer_norm_grad_kernel<E, 256, 1, 1, true>, 256);
+    } else if (units <= 512)
         go(layer_norm_grad_kernel<E, 256, 2, 1, true>, 256);
     else if (units <= 1024)
         go(layer_norm_grad_kernel<E, 512, 2, 1, true>, 512);

@@ -116,6 +116,23 @@ def test_gradients(rows, cols, dtype, pad):
     assert none is None and torch.equal(dx, dx2) and torch.equal(dw, dw2)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("cols", [8, 520, 1032, 1544, 2056, 4104, 8200, 12296])
+def test_gradients_at_every_end_of_a_row(cols, dtype):
+    """Last units of 1 to 7 elements, in each width that a kernel is made for; dx may be dy or dhidden there, too."""
+    for end in range(1, 8):
+        rows = 19 + end
+        test_gradients(rows, cols + end, dtype, 5)
+        gen = R.generator("ln ends", cols, end, dtype)
+        hid, w, dy, dh = (R.rows(gen, n, cols + end, dtype, 3) for n in (rows, 1, rows, rows))
+        stats = hid.float().mean(1), 1 / hid.float().std(1)
+        want = layer().tg_layer_norm_grad(dy, hid, w[0], *stats, dhidden=dh)
+        for place in (dy.clone(), dh.clone()):
+            other = {"dhidden": place} if torch.equal(place, dh) else {"dhidden": dh}
+            got = layer().tg_layer_norm_grad(dy if torch.equal(place, dh) else place, hid, w[0], *stats, dx=place, **other)
+            assert all(torch.equal(a, b) for a, b in zip(got, want, strict=True))
+
+
 def test_gradient_against_differences():
     gen = R.generator("ln differences")
     rows, cols, step = 3, 37, 1e-5
