@@ -38,6 +38,47 @@ struct NormArgs {
 
 __device__ inline int left_of(int cols, int col) { return cols - col; }  // <= 0: none
 
+// 16 bytes of a row as they lie; elements at or past `valid` are 0 and not read.
+template <typename E>
+__device__ inline i32x4 load_bits(const E *p, int valid) {
+    if (valid >= kUnitOf<E>) return ((const Global<Loose<i32x4, alignof(E)>> *)p)->v;
+    i32x4 r(0);
+#pragma unroll
+    for (int e = 0; e < kUnitOf<E>; ++e) {
+        if (e >= valid) continue;
+        if constexpr (sizeof(E) == 4)
+            r[e] = ((const Global<int> *)p)[e];
+        else
+            r[e / 2] |= (int)((unsigned)((const Global<unsigned short> *)p)[e] << (16 * (e % 2)));
+    }
+    return r;
+}
+// The same of a row's unit at `col` in one load: of a last unit that is not whole the
+// row's last 16 bytes, for in_place to move down when they are used.  (With a load and
+// a branch for each element of it 16384 x 1605 in bf16 took 119 us, so 64.)
+template <typename E>
+__device__ inline i32x4 load_unit(const E *row, int col, int valid) {
+    constexpr int kUnit = kUnitOf<E>;
+    if (valid <= 0) return i32x4(0);
+    if (col == 0 && valid < kUnit) return load_bits<E>(row, valid);
+    return ((const Global<Loose<i32x4, alignof(E)>> *)(row + col + std::min(valid, kUnit) - kUnit))->v;
+}
+template <typename E>
+__device__ inline void in_place(i32x4 &r, int col, int valid) {
+    if (valid <= 0 || valid >= kUnitOf<E> || col == 0) return;
+    const int bits = (kUnitOf<E> - valid) * (int)sizeof(E) * 8;
+    if (bits & 64) r = i32x4{r[2], r[3], 0, 0};
+    if (bits & 32) r = i32x4{r[1], r[2], r[3], 0};
+    if (sizeof(E) == 2 && (bits & 16)) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r[w] = (int)((unsigned)r[w] >> 16 | (w < 3 ? (unsigned)r[w + 1] << 16 : 0));
+    }
+}
+template <typename E>
+__device__ inline vec<float, kUnitOf<E>> floats(i32x4 bits) {
+    return __builtin_convertvector(__builtin_bit_cast(vec<E, kUnitOf<E>>, bits), vec<float, kUnitOf<E>>);
+}
+
 // Both reductions at once, in the order of block_reduce.
 struct Two {
     float a, b;
@@ -65,6 +106,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
     constexpr int kUnit = kUnitOf<E>;
     using unit = vec<float, kUnit>;
     constexpr int kRows = T == 64 ? 4 : 1;
+    constexpr bool kOneLoad = kCentre && !kStream;
     __shared__ float slots[2][T / 64];
     __shared__ Two pairs[T / 64];
     const int t = threadIdx.x % T;
@@ -103,7 +145,22 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
             for (int n = 0; n < N; ++n) f(h[n], t + n * T < units ? left_of(a.cols, (t + n * T) * kUnit) : 0);
         }
     };
-    if (!kStream) {
+    if constexpr (kOneLoad) {
+        i32x4 from[N], more[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int col = (t + n * T) * kUnit, left = t + n * T < units ? left_of(a.cols, col) : 0;
+            from[n] = load_unit<E>(x, col, left);
+            more[n] = r ? load_unit<E>(r, col, left) : i32x4(0);
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int col = (t + n * T) * kUnit, left = t + n * T < units ? left_of(a.cols, col) : 0;
+            in_place<E>(from[n], col, left), in_place<E>(more[n], col, left);
+            h[n] = floats<E>(from[n]);
+            if (r) h[n] += floats<E>(more[n]);
+        }
+    } else if (!kStream) {
 #pragma unroll
         for (int n = 0; n < N; ++n) h[n] = t + n * T < units ? read((t + n * T) * kUnit) : unit(0.0f);
     }
@@ -139,11 +196,17 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void norm_kernel(NormArgs a) {
     if (a.rstd && t == 0) a.rstd[row] = rstd;
 
     const auto normed = [&](unit v, int col) {
-        const unit w = load_f32<E, kUnit>(weight + col, left_of(a.cols, col));
-        unit y;
+        const int left = left_of(a.cols, col);
+        unit w, b(0.0f), y;
+        if constexpr (kOneLoad) {
+            i32x4 from = load_unit<E>(weight, col, left), more = bias ? load_unit<E>(bias, col, left) : i32x4(0);
+            in_place<E>(from, col, left), in_place<E>(more, col, left);
+            w = floats<E>(from), b = floats<E>(more);
+        } else {
+            w = load_f32<E, kUnit>(weight + col, left);
+            if (kCentre && bias) b = load_f32<E, kUnit>(bias + col, left);
+        }
         if constexpr (kCentre) {
-            unit b(0.0f);
-            if (bias) b = load_f32<E, kUnit>(bias + col, left_of(a.cols, col));
 #pragma unroll
             for (int e = 0; e < kUnit; ++e) y[e] = fmaf((v[e] - mean) * rstd, w[e], b[e]);
         } else {
