@@ -2,7 +2,7 @@
 // gradient (tg_layer_norm_grad); the forward kernels are norm.h's.
 //
 // Both are bound by memory as the root-mean-square norm's are.  8192 x 12288 in bf16
-// with a residual takes 145 to 153 us forward (5.3 to 5.6 TB/s) and 158 to 164 backward
+// with a residual takes 136 to 149 us forward (5.4 to 5.9 TB/s) and 156 to 164 backward
 // (5 TB/s), where a large copy reaches 4.8.
 #include "norm.h"
 

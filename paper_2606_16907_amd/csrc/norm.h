@@ -38,47 +38,6 @@ struct NormArgs {
 
 __device__ inline int left_of(int cols, int col) { return cols - col; }  // <= 0: none
 
-// 16 bytes of a row as they lie; elements at or past `valid` are 0 and not read.
-template <typename E>
-__device__ inline i32x4 load_bits(const E *p, int valid) {
-    if (valid >= kUnitOf<E>) return ((const Global<Loose<i32x4, alignof(E)>> *)p)->v;
-    i32x4 r(0);
-#pragma unroll
-    for (int e = 0; e < kUnitOf<E>; ++e) {
-        if (e >= valid) continue;
-        if constexpr (sizeof(E) == 4)
-            r[e] = ((const Global<int> *)p)[e];
-        else
-            r[e / 2] |= (int)((unsigned)((const Global<unsigned short> *)p)[e] << (16 * (e % 2)));
-    }
-    return r;
-}
-// The same of a row's unit at `col` in one load: of a last unit that is not whole the
-// row's last 16 bytes, for in_place to move down when they are used.  (With a load and
-// a branch for each element of it 16384 x 1605 in bf16 took 119 us, so 64.)
-template <typename E>
-__device__ inline i32x4 load_unit(const E *row, int col, int valid) {
-    constexpr int kUnit = kUnitOf<E>;
-    if (valid <= 0) return i32x4(0);
-    if (col == 0 && valid < kUnit) return load_bits<E>(row, valid);
-    return ((const Global<Loose<i32x4, alignof(E)>> *)(row + col + std::min(valid, kUnit) - kUnit))->v;
-}
-template <typename E>
-__device__ inline void in_place(i32x4 &r, int col, int valid) {
-    if (valid <= 0 || valid >= kUnitOf<E> || col == 0) return;
-    const int bits = (kUnitOf<E> - valid) * (int)sizeof(E) * 8;
-    if (bits & 64) r = i32x4{r[2], r[3], 0, 0};
-    if (bits & 32) r = i32x4{r[1], r[2], r[3], 0};
-    if (sizeof(E) == 2 && (bits & 16)) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) r[w] = (int)((unsigned)r[w] >> 16 | (w < 3 ? (unsigned)r[w + 1] << 16 : 0));
-    }
-}
-template <typename E>
-__device__ inline vec<float, kUnitOf<E>> floats(i32x4 bits) {
-    return __builtin_convertvector(__builtin_bit_cast(vec<E, kUnitOf<E>>, bits), vec<float, kUnitOf<E>>);
-}
-
 // Both reductions at once, in the order of block_reduce.
 struct Two {
     float a, b;
@@ -365,9 +324,9 @@ hipError_t launch_norm(NormArgs a, hipStream_t s) {
         go(norm_kernel<E, kEight, 512, 2, false, kCentre>, 512, 1);
     else if (units <= 1024)
         go(norm_kernel<E, kEight, 1024, 1, false, kCentre>, 1024, 1);
-    else if (kCentre && units <= 1536 && a.rows >= 256 && sizeof(E) == 2)  // 8192 x 12288: 153 us, by 768 threads 164
+    else if (kCentre && units <= 1536 && a.rows >= 256 && sizeof(E) == 2)  // 8192 x 12288: 149 us, by 768 threads 152
         go(norm_kernel<E, kEight, 512, 3, false, kCentre>, 512, 1);
-    else if (kCentre && units <= 1536)  // 3001 x 4999 of floats: 41.5 us, by 512 threads 45.5
+    else if (kCentre && units <= 1536)  // 8192 x 6000 of floats: 144 us, by 512 threads 153
         go(norm_kernel<E, kEight, 768, 2, false, kCentre>, 768, 1);
     else if (units <= 2048)
         go(norm_kernel<E, kEight, 1024, 2, false, kCentre>, 1024, 1);

@@ -2,8 +2,8 @@
 // row or of 128 rows (tg_quantize).
 //
 // Bound by memory: x is read once and stays in registers while its block's largest
-// value is found.  8192 x 28672 in bf16 takes 136 to 147 us by rows (4.8 to 5.2 TB/s)
-// and 133 by squares, where a large copy reaches 4.8.
+// value is found.  8192 x 28672 in bf16 takes 121 to 128 us by rows (5.5 to 5.8 TB/s)
+// and 131 by squares, where a large copy reaches 4.8.
 #include <algorithm>
 
 #include "layer_device.h"
@@ -90,21 +90,23 @@ __global__ __launch_bounds__(256) void quantize_rows(QuantizeArgs a) {
     const E *const x = (const E *)a.x + row * a.ldx;
     unsigned char *const y = a.y + row * a.ldy;
     char *const scales = (char *)a.scale + row * a.lds * (kPowers ? 1 : 4);
-    vec<float, kUnit> v[N];
+    i32x4 from[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const int64_t col = (unit0 + n * a.lanes) * kUnit;
-        v[n] = col < a.cols ? load_f32<E, kUnit>(x + col, (int)(a.cols - col)) : vec<float, kUnit>(0.0f);
+        from[n] = col < a.cols ? load_unit<E>(x, (int)col, (int)(a.cols - col)) : i32x4(0);
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const int64_t col = (unit0 + n * a.lanes) * kUnit;
+        if (col < a.cols) in_place<E>(from[n], (int)col, (int)(a.cols - col));
+        const vec<float, kUnit> v = floats<E>(from[n]);
         float most = 0.0f;
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e) most = fmaxf(most, finite_abs(v[n][e]));
+        for (int e = 0; e < kUnit; ++e) most = fmaxf(most, finite_abs(v[e]));
         const Scale s = scale_of<kPowers>(lanes_max<kLanes>(most));
         if (col >= a.cols) continue;
-        store_e4m3<kUnit>(y + col, divided<kPowers, kUnit>(v[n], s), (int)(a.cols - col));
+        store_e4m3<kUnit>(y + col, divided<kPowers, kUnit>(v, s), (int)(a.cols - col));
         if (t % kLanes == 0) store_scale<kPowers>(scales, col / kBlock, s);
     }
 }
@@ -118,15 +120,18 @@ __global__ __launch_bounds__(256) void quantize_squares(QuantizeArgs a) {
     const int64_t row0 = block / a.across * kBlock + threadIdx.x / kLanes;
     const int64_t b = block % a.across, col = b * kBlock + threadIdx.x % kLanes * kUnit;
     const int valid = (int)(a.cols - col);
+    i32x4 from[kN];
     vec<float, kUnit> v[kN];
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
         const int64_t row = row0 + n * kRows;
-        v[n] = row < a.rows && valid > 0 ? load_f32<E, kUnit>((const E *)a.x + row * a.ldx + col, valid) : vec<float, kUnit>(0.0f);
+        from[n] = row < a.rows && valid > 0 ? load_unit<E>((const E *)a.x + row * a.ldx, (int)col, valid) : i32x4(0);
     }
     float most = 0.0f;
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
+        if (valid > 0) in_place<E>(from[n], (int)col, valid);
+        v[n] = floats<E>(from[n]);
 #pragma unroll
         for (int e = 0; e < kUnit; ++e) most = fmaxf(most, finite_abs(v[n][e]));
     }
@@ -156,8 +161,8 @@ hipError_t launch_quantize(QuantizeArgs a, bool square, hipStream_t s) {
     for (a.lanes = kBlock / kUnitOf<E>; a.lanes < 256 && a.lanes < units;) a.lanes *= 2;
     const int64_t rows = ceil_div(a.rows, 256 / a.lanes);
     // Two units a thread (four of floats, which are half as long) where that leaves
-    // 1024 blocks: 8192 x 28672 in bf16 takes 147 us with two, 155 with four and 158 with
-    // one, 512 x 28672 10.9, 12.5 and 10.8, 8192^2 of floats 70, 67 and 78.
+    // 1024 blocks: 8192 x 28672 in bf16 takes 128 us with two, 137 with four and 147 with
+    // one, 512 x 28672 10.6, 11.5 and 11.6, 8192^2 of floats 68, 66 and 77.
     constexpr int kMany = sizeof(E) == 4 ? 4 : 2;
     const int n = units >= kMany * a.lanes && rows * ceil_div(units, kMany * a.lanes) >= 1024 ? kMany : 1;
     a.across = (int)ceil_div(units, n * a.lanes);
