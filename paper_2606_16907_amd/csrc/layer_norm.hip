@@ -4,6 +4,8 @@
 // Both are bound by memory as the root-mean-square norm's are.  8192 x 12288 in bf16
 // with a residual takes 136 to 149 us forward (5.4 to 5.9 TB/s) and 156 to 164 backward
 // (5 TB/s), where a large copy reaches 4.8.
+#include <type_traits>
+
 #include "norm.h"
 
 namespace tg {
@@ -67,15 +69,22 @@ __global__ __launch_bounds__(T *kRows) void layer_norm_grad_kernel(GradArgs a, E
         for (int n = 0; n < N; ++n) {
             const int col = (t + n * T) * kUnit, left = valid(n);
             if constexpr (kOneLoad) in_place<E>(now.g[n], col, left), in_place<E>(now.h[n], col, left), in_place<E>(now.more[n], col, left);
-            const unit g = floats<E>(now.g[n]), h = floats<E>(now.h[n]), w = floats<E>(weight[n]);
+            // past the row's end g is 0, and mean rstd may be an infinity
+            const auto add = [&](auto whole) {
+                const unit g = floats<E>(now.g[n]), h = floats<E>(now.h[n]), w = floats<E>(weight[n]);
 #pragma unroll
-            for (int e = 0; e < kUnit; ++e) {
-                const float xhat = (h[e] - now.mean) * now.rstd, gw = g[e] * w[e];
-                dw[n][e] = fmaf(g[e], xhat, dw[n][e]);
-                db[n][e] += g[e];
-                two.a += gw;
-                two.b = fmaf(gw, xhat, two.b);
-            }
+                for (int e = 0; e < kUnit; ++e) {
+                    const float xhat = whole || e < left ? (h[e] - now.mean) * now.rstd : 0.0f, gw = g[e] * w[e];
+                    dw[n][e] = fmaf(g[e], xhat, dw[n][e]);
+                    db[n][e] += g[e];
+                    two.a += gw;
+                    two.b = fmaf(gw, xhat, two.b);
+                }
+            };
+            if (left >= kUnit)
+                add(std::true_type{});
+            else if (left > 0)
+                add(std::false_type{});
             forget(now.g[n]), forget(now.h[n]), forget(weight[n]);
             __builtin_amdgcn_sched_barrier(0);  // a unit's floats at a time
         }

@@ -271,7 +271,8 @@ __global__ __launch_bounds__(1024) void norm_grad_stream(GradArgs a) {
         const unit w = load_f32<E, kUnit>((const E *)a.weight + col, valid);
 #pragma unroll
         for (int e = 0; e < kUnit; ++e) {
-            dot = fmaf(g[e] * w[e], (kCentre ? h[e] - centre : h[e]) * rstd, dot);
+            // past the row's end g is 0 and centre rstd may be an infinity
+            dot = fmaf(g[e] * w[e], kCentre ? (e < valid ? (h[e] - centre) * rstd : 0.0f) : h[e] * rstd, dot);
             if (kCentre) sum = fmaf(g[e], w[e], sum);
         }
     }
