@@ -19,13 +19,15 @@ __device__ inline f32x4 mma_block(i32x8 a, i32x8 b, f32x4 c, int code_a, int cod
 __device__ inline f32x4 mma_block(i32x8 a, i32x8 b) { return mma_block(a, b, f32x4(0.0f), 0, 0); }  // zeros: no scales
 
 // A buffer descriptor that moves through an operand: `bytes` further on, with as many
-// bytes fewer up to the operand's end.
+// bytes fewer up to the operand's end.  Its registers may come from vector
+// instructions; the pause stands before any load of this file (Stream::settle has why).
 __device__ inline i32x4 descriptor(uint64_t from, int64_t left) {
     i32x4 d;
     d[0] = __builtin_amdgcn_readfirstlane((int)from);
     d[1] = __builtin_amdgcn_readfirstlane((int)(from >> 32) & 0xffff);
     d[2] = __builtin_amdgcn_readfirstlane((int)std::min<int64_t>(left, 0x7ffffff0));
     d[3] = 0x00027000;
+    asm volatile("s_nop 4" : "+s"(d));
     return d;
 }
 __device__ inline void advance(i32x4 &d, int bytes) {
@@ -287,7 +289,6 @@ __global__ __launch_bounds__(512, 2) void product_blocks_large(Product a, Epilog
         i32x4 d_hi = descriptor((uint64_t)a.p + i0 * a.ldp + r0, (std::min<int64_t>(a.ni - i0, kB) - 1) * a.ldp + end_p - r0);
         i32x4 dq = descriptor((uint64_t)a.q + j0 * a.ldq + r0, (std::min<int64_t>(a.nj - j0, kB) - 1) * a.ldq + end_q - r0);
         const int last_p = (int)(end_p - r0 - (int64_t)(steps - 1) * kStepBytes), last_q = (int)(end_q - r0 - (int64_t)(steps - 1) * kStepBytes);
-        asm volatile("s_nop 4" : "+s"(d_hi), "+s"(dq));
         i32x4 d_lo = d_hi;
         const auto load_scales = [&](int g) {
             const unsigned to = lds + kScalesAt + g % 2 * kGroup;
