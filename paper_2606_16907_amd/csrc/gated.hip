@@ -295,8 +295,9 @@ tg_status tg_gated(const tg_gated_args *q, void *d_ws, size_t ws_bytes, tg_strea
     if (q->act < TG_ACT_NONE || q->act > TG_ACT_GELU) return call_failed(TG_EINVAL, "act %d", q->act);
     if (!gated_fits(q->m, q->n, q->k))
         return call_failed(TG_EINVAL, "m %lld, n %lld, k %lld", (long long)q->m, (long long)q->n, (long long)q->k);
-    const bool scaled = q->x_scale != nullptr;
-    if ((q->gate_scale != nullptr) != scaled || (q->up_scale != nullptr) != scaled || (scaled && q->type != TG_E4M3))
+    const bool scaled = q->x_scale || q->gate_scale || q->up_scale;
+    // those of no rows or columns may be NULL
+    if (scaled && (q->type != TG_E4M3 || (!q->x_scale && q->m > 0) || ((!q->gate_scale || !q->up_scale) && q->n > 0)))
         return call_failed(TG_EINVAL, "x_scale, gate_scale and up_scale come together, with 8-bit inputs");
     if ((q->gate != nullptr) != (q->up != nullptr)) return call_failed(TG_EINVAL, "gate and up are kept together");
     TG_TRY(check_matrix(q->x, q->ldx, q->m, q->k, q->type, "x"));

@@ -146,7 +146,8 @@ tg_status tg_linear(const tg_linear_args *q, void *d_ws, size_t ws_bytes, tg_str
     if (q->act < TG_ACT_NONE || q->act > TG_ACT_GELU) return call_failed(TG_EINVAL, "act %d", q->act);
     if (!sizes_fit(q->m, q->n, q->k))
         return call_failed(TG_EINVAL, "m %lld, n %lld, k %lld", (long long)q->m, (long long)q->n, (long long)q->k);
-    if ((q->x_scale != nullptr) != (q->w_scale != nullptr) || (q->x_scale && q->type != TG_E4M3))
+    // those of no rows or columns may be NULL
+    if ((q->x_scale || q->w_scale) && (q->type != TG_E4M3 || (!q->x_scale && q->m > 0) || (!q->w_scale && q->n > 0)))
         return call_failed(TG_EINVAL, "x_scale and w_scale come together, with 8-bit inputs");
     TG_TRY(check_matrix(q->x, q->ldx, q->m, q->k, q->type, "x"));
     TG_TRY(check_matrix(q->w, q->ldw, q->n, q->k, q->type, "w"));
