@@ -133,7 +133,7 @@ Product forward_product(const tg_gated_args &q) {
 // Both gradients' products in one launch, in tiles of 128, a place on each CU for
 // either: small ones leave half of the GPU idle by themselves.  1531 x 1001 x 1367 in
 // f16 takes 29 us, and what comes after it 5, where two launches took 19 and 18 and
-// theirs 8.  plan_grad takes whichever cut_tail estimates to be shorter.
+// theirs 8.  cut_gradients chooses.
 struct OneOfTwo {
     Product a;
     Epilogue e;
@@ -212,15 +212,8 @@ GatedGradPlan plan_grad(const tg_gated_grad_args &q, char *ws) {
     p.pack_x = p.weights && !streams(p.dw.q, p.dw.ldq, 2, 0, true);
     p.w_bytes = p.pack_w ? round256(q.n * packed_k) : 0;
     p.x_bytes = p.pack_x ? round256(q.m * packed_k) : 0;
-    if (q.dx) p.cut_dx = cut_tail(p.dx.ni, p.dx.nj, p.dx.nr, 2);
-    if (p.weights) p.cut_dw = cut_tail(p.dw.ni, p.dw.nj, p.dw.nr, 2);
-    if (q.dx && p.weights) {
-        const TailCut dx = cut_tail(p.dx.ni, p.dx.nj, p.dx.nr, 2, true), dw = cut_tail(p.dw.ni, p.dw.nj, p.dw.nr, 2, true);
-        p.two = std::max(dx.us, dw.us) < p.cut_dx.us + p.cut_dw.us;
-        // a grid holds fewer than 2^32 threads, 256 a block
-        p.two = p.two && dx.whole + dx.tail * dx.splits + dw.whole + dw.tail * dw.splits < (1 << 24);
-        if (p.two) p.cut_dx = dx, p.cut_dw = dw;
-    }
+    const GradCut c = cut_gradients(q.m, q.k, ldz, p.dw.ni, q.dx, p.weights);
+    p.cut_dx = c.dx, p.cut_dw = c.dw, p.two = c.two;
     p.dx_bytes = round256(p.cut_dx.bytes());
     p.dw_bytes = round256(p.cut_dw.bytes());
     if (!p.two && p.dx_bytes && p.dw_bytes) p.dx_bytes = std::max(p.dx_bytes, p.dw_bytes), p.dw_bytes = 0;  // one after the other

@@ -1095,30 +1095,6 @@ struct Plan {
 // floats, where 16 bits take 0.58.
 template <Form kForm>
 constexpr double pace_of(int size) { return kForm == kBlocks ? 1.4 : kForm == kExponents ? 1.25 : size == 1 ? 1.1 : 1.0; }
-// Rows of x up to which product_few is faster than tiles, with two weights or scaled
-// blocks, each with `columns` sums in all and rows of row_bytes.  Up to 16 it reads as
-// much: 16 rows through 7168 x 4096 take 12.6 us with scaled blocks and 11.5 gated in 8
-// bits, in tiles 17.5 and 17.2; through 4096 x 14336 23 and 21, in tiles 23 and 19; from
-// 100 MB on 12 rows (16384 x 16384: 75 for 75, 16 rows 84 for 76).  Up to 8192 columns
-// tiles are few and split, which is another launch: 32 rows through 7168 x 4096 take
-// 15.8 for 17.9, through 4096 x 4096 10.3 for 16.8, 64 rows through 2048 x 2048 9.8 for
-// 19.2; longer rows are slower (64 through 7168 x 2048: 20.3 for 19.4).
-inline int64_t few_rows(int64_t columns, int64_t row_bytes) {
-    const int64_t all = columns * row_bytes;
-    if (columns <= 8192 && row_bytes <= 4096 && all <= 17000000) return 64;
-    if (columns <= 8192 && row_bytes <= 8192 && all <= 30000000) return 32;
-    return all <= 100000000 ? 16 : 12;
-}
-// The same where an operand would have to be packed first.  Rows at multiples of 4 bytes
-// are read as fast as others: 32 through 7169 x 7169 take 31 us for 44, through 4097 x
-// 20002 43 for 62, through 16385 x 4098 50 for 53; rows that are not, the slower the
-// longer: 32 through 4098 x 289 17 for 19, 16 through 10486 x 2289 28.5 for 29.6, 8
-// through 8190 x 16390 111 for 89.
-inline int64_t few_packed_rows(int64_t columns, int64_t row_bytes, bool words) {
-    const int64_t all = std::max<int64_t>(1, columns * row_bytes);
-    const int64_t most = words ? 20 + 900000000 / all : std::min(130000 / std::max<int64_t>(1, row_bytes), 2 + 500000000 / all);
-    return std::max<int64_t>(1, std::min<int64_t>(64, most));
-}
 template <Form kForm = kOne>
 Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bool down_q) {
     Plan p{};
