@@ -106,13 +106,17 @@ inline int64_t few_rows(int64_t columns, int64_t row_bytes) {
     return all <= 100000000 ? 16 : 12;
 }
 // The same where an operand would have to be packed first.  Rows at multiples of 4 bytes
-// are read as fast as others: 32 through 7169 x 7169 take 31 us for 44, through 4097 x
-// 20002 43 for 62, through 16385 x 4098 50 for 53; rows that are not, the slower the
-// longer: 32 through 4098 x 289 17 for 19, 16 through 10486 x 2289 28.5 for 29.6, 8
-// through 8190 x 16390 111 for 89.
+// are read as fast as others: 48 through 7169 x 7169 take 39 us for 44, 32 through 4097 x
+// 20002 43 for 62 (48 of gated operands 57 for 51), 32 through 16385 x 4098 50 for 53, of
+// gated ones 50 for 47, 24 42 for 46; 64 through 40966 bytes x 512 24 for 41.  Over 198
+// sizes the limits are 0.1% from the faster of both in the mean and 5% at worst.  Rows
+// that are not, the slower the longer: 4098 x 289 up to some 38 rows (32 take 17 us for
+// 19, 48 22 for 20), 10486 x 2289 up to some 14 (8 take 24 for 29, 24 37 for 29), 8190 x
+// 16390 up to fewer than 8 (111 for 89).
 inline int64_t few_packed_rows(int64_t columns, int64_t row_bytes, bool words) {
     const int64_t all = std::max<int64_t>(1, columns * row_bytes);
-    const int64_t most = words ? 20 + 900000000 / all : std::min(130000 / std::max<int64_t>(1, row_bytes), 2 + 500000000 / all);
+    if (words) return all <= 25000000 ? 64 : row_bytes > 16384 ? 24 : all <= 60000000 ? 48 : 32;
+    const int64_t most = std::min(130000 / std::max<int64_t>(1, row_bytes), 2 + 500000000 / all);
     return std::max<int64_t>(1, std::min<int64_t>(64, most));
 }
 

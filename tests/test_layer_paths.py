@@ -99,3 +99,15 @@ FEW = [(1, 28672, 8192, True), (16, 10000, 8192, True), (24, 9000, 4096, False),
 @pytest.mark.parametrize("m,columns,row_bytes,few", FEW)
 def test_few_rows(ask, m, columns, row_bytes, few):
     assert (m <= ask("few", columns, row_bytes)[0]) == few
+
+
+# rows whose operands would have to be packed first: columns of the sums, bytes of a row, whether rows start at multiples of 4
+# bytes, rows up to which product_few measured as fast or faster, and the least number of rows from which it was 6% slower
+PACKED = [(7169, 7169, True, 48, 64), (20002, 4097, True, 32, 64), (4098, 16385, True, 24, 48), (2048, 32770, True, 24, 32), (3584, 14338, True, 48, 65),
+          (8194, 16382, True, 32, 48), (512, 40966, True, 64, 65), (8193, 2049, True, 64, 65), (289, 4098, False, 31, 48), (2289, 10486, False, 8, 24),
+          (16390, 8190, False, 1, 8), (16390, 8191, False, 1, 8)]
+
+
+@pytest.mark.parametrize("columns,row_bytes,words,faster,slower", PACKED)
+def test_few_rows_that_would_be_packed(ask, columns, row_bytes, words, faster, slower):
+    assert faster <= ask("packed", columns, row_bytes, words)[0] < slower
