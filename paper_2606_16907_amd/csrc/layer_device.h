@@ -13,6 +13,14 @@ namespace tg {
 tg_status call_failed(tg_status st, const char *fmt, ...);
 tg_status device_failed(hipError_t e, const char *what);
 
+#define TG_TRY(call)                  \
+    do {                              \
+        const tg_status st_ = (call); \
+        if (st_ != TG_OK) return st_; \
+    } while (0)
+
+inline size_t size_of(int type) { return type == TG_F32 ? 4 : type == TG_E4M3 ? 1 : 2; }
+
 using bf16 = __bf16;
 using f16 = _Float16;
 struct e4m3 {

@@ -351,7 +351,6 @@ void launch_grad_stream(GradArgs a, int blocks, hipStream_t s) {
         hipLaunchKernelGGL((norm_grad_stream<E, kCentre>), dim3((unsigned)std::min(kMostBlocks, a.rows - a.first)), dim3(1024), 0, s, a);
 }
 
-inline size_t size_of(int type) { return type == TG_F32 ? 4 : type == TG_E4M3 ? 1 : 2; }
 inline bool norm_type(int type) { return type == TG_F32 || type == TG_BF16 || type == TG_F16; }
 
 inline tg_status check_rows(const void *p, int64_t ld, int64_t rows, int64_t cols, int type, const char *what) {
@@ -366,12 +365,6 @@ inline tg_status check_sizes(int64_t rows, int64_t cols) {
         return call_failed(TG_EINVAL, "rows %lld, cols %lld", (long long)rows, (long long)cols);
     return TG_OK;
 }
-
-#define TG_TRY(call)                  \
-    do {                              \
-        const tg_status st_ = (call); \
-        if (st_ != TG_OK) return st_; \
-    } while (0)
 
 }  // namespace
 }  // namespace tg

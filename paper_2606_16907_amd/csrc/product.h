@@ -66,8 +66,12 @@ struct Epilogue {
     void *out, *pre;
     int64_t ldr, ldo, ldp;
     int act;
-    float *partial;  // [splits, ni, nj] sums over a share of r, which join_kernel finishes; NULL: finished at once
-    // the second matrix's (kGated: columns nj and on of a row of `partial`; kHalves: out)
+    // Sums over shares of r.  Where all of C is shared out (kOne, product_few): [splits, ni,
+    // nj], of kGated [splits, ni, 2 nj], up's columns behind gate's, which join_kernel
+    // finishes; NULL: finished at once.  After a tail cut: [tile of the tail][share], each a
+    // whole tile row by row, of kGated gate's half of a row and then up's, for join_body.
+    float *partial;
+    // the second matrix's (kHalves: out)
     const float *w_scale2;
     const void *bias2;
     void *out2, *pre2;
@@ -981,8 +985,6 @@ __global__ __launch_bounds__(256) void join_kernel(Epilogue e, int splits, int64
     };
     if constexpr (kForm == kGated)
         finish_gated<O, 8>(sum(j), sum(nj + j), i, j, valid, e);
-    else if constexpr (kForm == kHalves)
-        finish_halves<O, 8>(sum(j), i, j, valid, e);
     else
         finish<O, 8>(sum(j), i, j, valid, e);
 }
@@ -1082,8 +1084,9 @@ inline bool streams(const void *p, int64_t ld, int size, int64_t r_bytes, bool d
 }
 inline int64_t whole_ld(int64_t cols, int size) { return ceil_div(cols * size, 16) * 16 / size; }
 
-// How a product is done: the kernel, the operands that are packed first, and what
-// lies where in the workspace: packed P, packed Q (both of its matrices), shares.
+// How a product of one call is done (kOne, kGated, kBlocks and kExponents): the kernel,
+// the operands that are packed first, and what lies where in the workspace: packed P,
+// packed Q (both of its matrices), shares.
 struct Plan {
     bool few, pack_p, pack_q;
     Cut cut;       // kOne, and `few`
@@ -1099,11 +1102,10 @@ template <Form kForm = kOne>
 Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bool down_q) {
     Plan p{};
     if (a.ni == 0 || a.nj == 0) return p;
-    constexpr bool kTwo = kForm == kGated || kForm == kSeam;
-    const int64_t columns = kForm == kGated ? 2 * a.nj : a.nj;  // of the sums
+    constexpr bool kPair = kForm == kGated;
+    const int64_t columns = kPair ? 2 * a.nj : a.nj;  // of the sums
     p.pack_p = !streams(a.p, a.ldp, size, r_bytes_p, down_p);
-    p.pack_q = !streams(a.q, a.ldq, size, a.nr * size, down_q) || (kTwo && !streams(a.q2, a.ldq2, size, a.nr * size, down_q)) ||
-               (kForm == kSeam && a.ldq != a.ldq2);
+    p.pack_q = !streams(a.q, a.ldq, size, a.nr * size, down_q) || (kPair && !streams(a.q2, a.ldq2, size, a.nr * size, down_q));
     // From some 8 rows on tiles of 128 and splits are as fast with one weight: 4096 x
     // 14336 in bf16, 25 us for one row against 28, 28 for both at 8, 34 against 28 at
     // 16.  Where an operand would have to be packed, up to 64 rows.
@@ -1111,7 +1113,7 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
     int64_t most_few = packs ? 64 : 8;
     if (kForm != kOne) {
         const auto words = [&](const void *q, int64_t ld) { return ((uintptr_t)q | (uintptr_t)(ld * size)) % 4 == 0; };
-        most_few = packs ? few_packed_rows(columns, a.nr * size, words(a.p, a.ldp) && words(a.q, a.ldq) && (!kTwo || words(a.q2, a.ldq2)))
+        most_few = packs ? few_packed_rows(columns, a.nr * size, words(a.p, a.ldp) && words(a.q, a.ldq) && (!kPair || words(a.q2, a.ldq2)))
                          : few_rows(columns, a.nr * size);
     }
     p.few = !down_p && !down_q && a.ni <= most_few;
@@ -1135,7 +1137,7 @@ Plan plan_product(const Product &a, int size, int64_t r_bytes_p, bool down_p, bo
         p.tail = cut_tail(a.ni, columns, a.nr, size, false, pace_of<kForm>(size));
     const auto packed = [&](int64_t n, int64_t r, bool down) { return round256(down ? r * whole_ld(n, size) * size : n * whole_ld(r, size) * size); };
     p.p_bytes = p.pack_p ? packed(a.ni, a.nr, down_p) : 0;
-    p.q_bytes = p.pack_q ? packed(a.nj, kForm == kSeam ? a.half : a.nr, down_q) * (kTwo ? 2 : 1) : 0;
+    p.q_bytes = p.pack_q ? packed(a.nj, a.nr, down_q) * (kPair ? 2 : 1) : 0;
     p.bytes = p.p_bytes + p.q_bytes + (kForm == kOne ? cut_bytes(p.cut, a.ni, columns) : round256(p.tail.bytes()));
     return p;
 }
@@ -1154,19 +1156,18 @@ hipError_t join(const Product &a, const Epilogue &e, int splits, hipStream_t s) 
 template <typename T, Form kForm, bool kDownP, bool kDownQ>
 hipError_t pack_operands(Product &a, const Plan &p, int64_t &r_bytes_p, char *ws, hipStream_t s) {
     constexpr int kSize = sizeof(T);
-    constexpr bool kTwo = kForm == kGated || kForm == kSeam;
+    constexpr bool kPair = kForm == kGated;
     if (!(p.pack_p || p.pack_q) || a.nr == 0) return hipSuccess;
     Packing k{};
     const auto pack = [&](int o, const void *&from, int64_t &ld, int64_t n, int64_t r, bool down, char *to) {
         pack_operand(k, o, from, ld, down ? r : n, down ? n : r, kSize, to);
     };
-    const int64_t r_q = kForm == kSeam ? a.half : a.nr;
     if (p.pack_p) pack(0, a.p, a.ldp, a.ni, a.nr, kDownP, ws), r_bytes_p = a.ldp * kSize;
-    if (p.pack_q) pack(1, a.q, a.ldq, a.nj, r_q, kDownQ, ws + p.p_bytes);
-    if (p.pack_q && kTwo) pack(2, a.q2, a.ldq2, a.nj, r_q, kDownQ, ws + p.p_bytes + p.q_bytes / 2);
+    if (p.pack_q) pack(1, a.q, a.ldq, a.nj, a.nr, kDownQ, ws + p.p_bytes);
+    if (p.pack_q && kPair) pack(2, a.q2, a.ldq2, a.nj, a.nr, kDownQ, ws + p.p_bytes + p.q_bytes / 2);
     const int64_t units = std::max({k.rows[0] * k.ld_to[0], k.rows[1] * k.ld_to[1], k.rows[2] * k.ld_to[2]}) * kSize / 16;
     using Moved = std::conditional_t<kSize == 1, unsigned char, T>;
-    const dim3 grid((unsigned)std::min<int64_t>(2048, ceil_div(units, 256)), kTwo ? 3 : 2);
+    const dim3 grid((unsigned)std::min<int64_t>(2048, ceil_div(units, 256)), kPair ? 3 : 2);
     hipLaunchKernelGGL(pack_kernel<Moved>, grid, dim3(256), 0, s, k);
     return hipGetLastError();
 }
@@ -1206,7 +1207,6 @@ hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hi
     constexpr int kSize = sizeof(T);
     if (a.ni == 0 || a.nj == 0) return hipSuccess;
     const Plan p = plan_product<kForm>(a, kSize, r_bytes_p, kDownP, kDownQ);
-    e.seam = a.seam, e.half = a.half;
     if constexpr (!kDownP && !kDownQ) {
         if (p.few) return launch_few<T, O, kForm>(a, e, p, ws, s);
     }
@@ -1231,8 +1231,6 @@ hipError_t launch_product(Product a, Epilogue e, int64_t r_bytes_p, char *ws, hi
 // ---------------------------------------------------------------------------
 // checks and sizes on the host
 // ---------------------------------------------------------------------------
-inline size_t size_of(int type) { return type == TG_F32 ? 4 : type == TG_E4M3 ? 1 : 2; }
-
 inline tg_status check_matrix(const void *p, int64_t ld, int64_t rows, int64_t cols, int type, const char *what) {
     if (rows == 0 || cols == 0) return TG_OK;
     if (!p) return call_failed(TG_EINVAL, "%s is NULL", what);
@@ -1268,12 +1266,6 @@ inline int slope_rows(int64_t m, int64_t n) {  // blocks down the rows: about 20
     const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, ceil_div(n, 256)));
     return (int)std::min<int64_t>(want, std::max<int64_t>(1, ceil_div(m, 8)));
 }
-
-#define TG_TRY(call)                  \
-    do {                              \
-        const tg_status st_ = (call); \
-        if (st_ != TG_OK) return st_; \
-    } while (0)
 
 }  // namespace
 }  // namespace tg
