@@ -8,10 +8,7 @@
 // (N of them), every load of the row in flight before the reduction.  8192 x 8192
 // in bf16 takes 89 us forward (6.0 TB/s), as much with 8 bits out, and 117
 // backward (4.6 TB/s), where a large copy reaches 4.8 to 4.9; forward with 256
-// threads a row took 96, backward with 768 or 1024 blocks 24 and 11 more in all,
-// with the next row fetched ahead the same.  The gradient of short rows is bound
-// by latency instead: its 512 blocks have a wave each up to 64 units a row, and
-// 16384 x 512 in bf16 takes 47 us, 1.4 TB/s.
+// threads a row took 96.
 //
 // hidden is h rounded once to the inputs' type, which is what the next operator
 // and the gradient read; y is of the h before that rounding.  In 16 bits with a

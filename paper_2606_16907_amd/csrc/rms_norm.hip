@@ -8,6 +8,9 @@ namespace {
 // A block takes rows blockIdx.x, + gridDim.x, ... and keeps its columns' share of
 // dweight in registers over all of them; one row of sums a block leaves it.  The
 // weight stays in registers too, except in blocks of 1024, whose threads have 128.
+// 8192 x 8192 in bf16 with 768 or 1024 blocks took 24 and 11 us more than with 512, with
+// the next row fetched ahead the same.  Short rows are bound by latency: the 512 blocks
+// have a wave each up to 64 units a row, and 16384 x 512 in bf16 takes 47 us, 1.4 TB/s.
 template <typename E, int T, int N>
 __global__ __launch_bounds__(T) void norm_grad_kernel(GradArgs a) {
     constexpr int kUnit = kUnitOf<E>;
